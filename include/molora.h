@@ -67,6 +67,11 @@ enum {
 #define MOLORA_MAX_BREAKS 64    /* M of molora_route_vocab             */
 #define MOLORA_MAX_HIDDEN 256   /* H of molora_route_mlp, a multiple of 8 */
 #define MOLORA_MAX_TOPK 4       /* k of molora_route_mlp / molora_apply_mix */
+#define MOLORA_BF16 0           /* src_type of molora_mx_quantize   */
+#define MOLORA_F32 1
+#define MOLORA_ACT_SILU 0       /* act of molora_apply_gated: g / (1 + e^-g)                         */
+#define MOLORA_ACT_GELU 1       /* g Phi(g), Phi the normal distribution function                    */
+#define MOLORA_ACT_GELU_TANH 2  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                 */
 #define MOLORA_STATIC_WORKSPACE_BYTES (8u << 20) /* scratch of molora_apply_static, per GPU */
 
 /*
@@ -420,6 +425,88 @@ molora_status molora_apply_mix(const void *x, const void *W, const void *A, cons
                                const int32_t *idx, const float *w, const int32_t *slots, float *h,
                                int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank,
                                int32_t k, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * 4-bit microscaled floating point: quantisation and product.  Values are grouped in blocks of 32
+ * along k; a block holds a power of two 2^X and 32 codes of 1 sign, 2 exponent and 1 mantissa bit
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives):
+ *
+ *     X = floor(log2 max |v|) - 2, at least -127;   code = the nearest to v 2^-X, the even one in
+ *     the middle between two, 6 where it is larger;   a block with a NaN or an infinity stands for NaN
+ *
+ * An operand of `rows` rows and K columns (the rows of x; of a base weight W [d_in][d_out] its
+ * d_out columns, K = d_in) is stored in the order in which the matrix instructions take it:
+ *     codes   [rows / 16][K / 128][64][16] bytes: entry 16 b + i of a tile is block b of row i, its
+ *             32 codes in ascending k, the even one in the low half of a byte
+ *     scales  [rows / 16][K / 512][64][4] bytes: X + 127 of entry 16 b + i for four k tiles of 128
+ *             (255: NaN)
+ * with rows, K / 128 and K / 512 rounded up and zero bytes in what that adds.  The two size functions
+ * return the bytes of either (0 if the sizes are invalid: K >= 8 and a multiple of 8, and fewer than 2^24
+ * tiles of 16 x 128).
+ *
+ * molora_mx_quantize     rows of src, bf16 (MOLORA_BF16) or fp32 (MOLORA_F32) [rows][K]
+ * molora_mx_quantize_w   a base weight W bf16 [d_in][d_out] (d_out a multiple of 8); once per weight
+ * molora_mx_dequantize   the values that the blocks stand for, dst fp32 [rows][K]
+ * molora_mx_matmul       h = Q(x) Q(W), fp32 [N][d_out]: products of the values that the blocks
+ *                        stand for, added in fp32; xc, xs of N rows, wc, ws of molora_mx_quantize_w
+ * molora_apply_mx        molora_apply on such a base weight: h[i] = Q(x[i]) Q(W) + (x[i] A_r) B_r.
+ *                        x is given in bf16: the base product takes its 4-bit blocks (made inside), the
+ *                        adapters x itself.  workspace as for molora_apply, of
+ *                        molora_apply_mx_workspace_bytes(...) bytes, which never decrease with N.
+ * All pointers DEVICE, 16-byte aligned (workspace 256).  Errors as molora_apply.
+ */
+size_t molora_mx_codes_bytes(int64_t rows, int32_t K);
+size_t molora_mx_scales_bytes(int64_t rows, int32_t K);
+molora_status molora_mx_quantize(const void *src, int32_t src_type, void *codes, void *scales,
+                                 int64_t rows, int32_t K, void *stream);
+molora_status molora_mx_quantize_w(const void *W, void *codes, void *scales, int32_t d_in,
+                                   int32_t d_out, void *stream);
+molora_status molora_mx_dequantize(const void *codes, const void *scales, float *dst, int64_t rows,
+                                   int32_t K, void *stream);
+molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, const void *ws, float *h,
+                               int64_t N, int32_t d_in, int32_t d_out, void *stream);
+size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank);
+molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, const void *A,
+                              const void *B, const int32_t *r, float *h, int64_t N, int32_t d_in,
+                              int32_t d_out, int32_t C, int32_t rank, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * The gated feed-forward block with routed adapters: gate and up projection, activation and product.
+ *
+ *     h = x W + (x A_r) B_r,   W [d_in][2 F] = [gate | up],   z = act(h[:, :F]) * h[:, F:]
+ *
+ * h is what molora_apply gives for these operands with d_out = 2 F (separate adapters of the two
+ * projections are one of the sum of their ranks, B block-diagonal).  z DEVICE bf16 [N][F] is ready to be
+ * the x of a down projection.  From 65 tokens on z is made in the epilogue of the one GEMM, and h is
+ * never stored unless pre (DEVICE fp32 [N][2 F], may be NULL) asks for it: the backward pass needs it.
+ * Without adapters: A, B, r NULL, C = rank = 0.  act: MOLORA_ACT_*.  F >= 8 and a multiple of 8; x, W
+ * and h in bf16 below 4 GiB each.  workspace DEVICE, 256-byte aligned, of
+ * molora_apply_gated_workspace_bytes(...) bytes (0 and NULL without adapters), never less for
+ * more tokens.  Errors as molora_apply.
+ *
+ * molora_gated_backward: the gradients of a scalar loss whose gradient with respect to z is dz (DEVICE bf16
+ * [N][F]).  With dh = [dz u act'(g) | dz act(g)], [g | u] = pre, t = x A_r and s = dh B_r^T:
+ *
+ *     dx = dh W^T + s A_r^T     dW = x^T dh     dA_c = x_c^T s_c     dB_c = t_c^T dh_c
+ *
+ * (the subscript c: the tokens with r = c; adapters without tokens get zeros).  dx [N][d_in], dW [d_in][2 F],
+ * dA [C][d_in][rank], dB [C][rank][2 F] DEVICE bf16, each written whole, rounded once from fp32
+ * sums; a NULL one is not computed (dA and dB have to be NULL without adapters).  dh is rounded to
+ * bf16 before these products.  workspace as above, of
+ * molora_gated_backward_workspace_bytes(...) bytes, which never decrease with N.
+ */
+size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank);
+molora_status molora_apply_gated(const void *x, const void *W, const void *A, const void *B,
+                                 const int32_t *r, void *z, float *pre, int64_t N, int32_t d_in, int32_t F,
+                                 int32_t C, int32_t rank, int32_t act, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank);
+molora_status molora_gated_backward(const void *dz, const void *x, const void *W, const void *A,
+                                    const void *B, const int32_t *r, const float *pre, void *dx, void *dW,
+                                    void *dA, void *dB, int64_t N, int32_t d_in, int32_t F, int32_t C,
+                                    int32_t rank, int32_t act, void *workspace, size_t workspace_bytes,
+                                    void *stream);
 
 /*
  * Replayable launch sequences (Sec. "CUDA Graph Compatibility": fixed shapes and fixed

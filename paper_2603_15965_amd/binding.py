@@ -23,6 +23,10 @@ EXPORTS = ["molora_route", "molora_route_vocab", "molora_bucket", "molora_apply_
            "molora_route_mlp_workspace_bytes", "molora_route_mlp", "molora_route_compose",
            "molora_gate_dispatch",
            "molora_apply_mix_workspace_bytes", "molora_apply_mix",
+           "molora_mx_codes_bytes", "molora_mx_scales_bytes", "molora_mx_quantize", "molora_mx_quantize_w",
+           "molora_mx_dequantize", "molora_mx_matmul", "molora_apply_mx_workspace_bytes", "molora_apply_mx",
+           "molora_apply_gated_workspace_bytes", "molora_apply_gated", "molora_gated_backward_workspace_bytes",
+           "molora_gated_backward",
            "molora_graph_begin", "molora_graph_end", "molora_graph_launch", "molora_graph_destroy",
            "molora_launch_timer_create", "molora_launch_timer_arm", "molora_launch_timer_elapsed_us",
            "molora_launch_timer_destroy",
@@ -113,6 +117,28 @@ def load():
     lib.molora_apply_mix_workspace_bytes.restype = sz
     lib.molora_apply_mix.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
     lib.molora_apply_mix.restype = ctypes.c_int
+    for f in (lib.molora_mx_codes_bytes, lib.molora_mx_scales_bytes):
+        f.argtypes = [i64, i32]
+        f.restype = sz
+    lib.molora_mx_quantize.argtypes = [vp, i32, vp, vp, i64, i32, vp]
+    lib.molora_mx_quantize.restype = ctypes.c_int
+    lib.molora_mx_quantize_w.argtypes = [vp, vp, vp, i32, i32, vp]
+    lib.molora_mx_quantize_w.restype = ctypes.c_int
+    lib.molora_mx_dequantize.argtypes = [vp, vp, vp, i64, i32, vp]
+    lib.molora_mx_dequantize.restype = ctypes.c_int
+    lib.molora_mx_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, vp]
+    lib.molora_mx_matmul.restype = ctypes.c_int
+    lib.molora_apply_mx_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.molora_apply_mx_workspace_bytes.restype = sz
+    lib.molora_apply_mx.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, sz, vp]
+    lib.molora_apply_mx.restype = ctypes.c_int
+    for f in (lib.molora_apply_gated_workspace_bytes, lib.molora_gated_backward_workspace_bytes):
+        f.argtypes = [i64, i32, i32, i32, i32]
+        f.restype = sz
+    lib.molora_apply_gated.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
+    lib.molora_apply_gated.restype = ctypes.c_int
+    lib.molora_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
+    lib.molora_gated_backward.restype = ctypes.c_int
     lib.molora_graph_begin.argtypes = [vp]
     lib.molora_graph_begin.restype = ctypes.c_int
     lib.molora_graph_end.argtypes = [vp, ctypes.POINTER(vp)]
@@ -672,6 +698,167 @@ def molora_apply_mix(x, W, A, B, idx, w=None, slots=None, C=None, h=None, worksp
         _opt(slots, torch.int32, "slots", (C,)), _dev(h, torch.float32, "h", (N, d_out)),
         N, d_in, d_out, C, rank, k, ws, ws_bytes, _stream(stream))
     return h
+
+
+def _call_here(fn, *args):
+    """_call for the operators below, whose launches go to the current device: tensors of another one are
+    refused (their addresses mean nothing there)."""
+    if _raw_device is not None and torch.cuda.is_initialized():
+        here = _raw_device()
+        for a in args:
+            if type(a) is tuple and isinstance(a[0], _Tensor) and a[0].is_cuda and a[0].get_device() != here:
+                raise ValueError(f"{a[2]} is on cuda:{a[0].get_device()}, the current device is cuda:{here}")
+    _call(fn, *args)
+
+
+def _mx_shapes(rows, K):
+    """Shapes of the codes and scales of a microscaled operand."""
+    if rows < 0 or K < 8 or K % 8 != 0:
+        raise ValueError(f"a microscaled operand has K >= 8, a multiple of 8: got {rows} rows of {K}")
+    tiles = -(-rows // 16)
+    return (tiles, -(-K // 128), 64, 16), (tiles, -(-K // 512), 64, 4)
+
+
+def _mx_outputs(rows, K, codes, scales, device):
+    c, s = _mx_shapes(rows, K)
+    if codes is None:
+        codes = torch.empty(c, dtype=torch.uint8, device=device)
+    if scales is None:
+        scales = torch.empty(s, dtype=torch.uint8, device=device)
+    return codes, scales
+
+
+def _mx(codes, scales, rows, K, name):
+    c, s = _mx_shapes(rows, K)
+    return _dev(codes, torch.uint8, f"{name} codes", c), _dev(scales, torch.uint8, f"{name} scales", s)
+
+
+def molora_mx_quantize(x, codes=None, scales=None, stream=None):
+    """Rows of x (bf16 or fp32) to 4-bit blocks of 32 along the row: (codes, scales), uint8."""
+    rows, K = _two(x, "x")
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"x must be bfloat16 or float32, got {x.dtype}")
+    codes, scales = _mx_outputs(rows, K, codes, scales, x.device)
+    _call_here("molora_mx_quantize", _dev(x, x.dtype, "x"), int(x.dtype is torch.float32), *_mx(codes, scales, rows, K, "x"), rows, K,
+          _stream(stream))
+    return codes, scales
+
+
+def molora_mx_quantize_w(W, codes=None, scales=None, stream=None):
+    """A base weight W [d_in][d_out] (bf16) to 4-bit blocks along d_in: (codes, scales), done once."""
+    d_in, d_out = _two(W, "W")
+    codes, scales = _mx_outputs(d_out, d_in, codes, scales, W.device)
+    _call_here("molora_mx_quantize_w", _dev(W, torch.bfloat16, "W"), *_mx(codes, scales, d_out, d_in, "W"), d_in, d_out, _stream(stream))
+    return codes, scales
+
+
+def molora_mx_dequantize(codes, scales, rows, K, out=None, stream=None):
+    """The values that the blocks stand for, fp32 [rows][K] (of a base weight: [d_out][d_in])."""
+    rows, K = int(rows), int(K)
+    args = _mx(codes, scales, rows, K, "operand")
+    if out is None:
+        out = torch.empty((rows, K), dtype=torch.float32, device=codes.device)
+    _call_here("molora_mx_dequantize", *args, _dev(out, torch.float32, "out", (rows, K)), rows, K, _stream(stream))
+    return out
+
+
+def molora_mx_matmul(xc, xs, wc, ws, N, d_in, d_out, h=None, stream=None):
+    """h = Q(x) Q(W), fp32 [N][d_out], of operands from molora_mx_quantize and molora_mx_quantize_w."""
+    N, d_in, d_out = int(N), int(d_in), int(d_out)
+    args = (*_mx(xc, xs, N, d_in, "x"), *_mx(wc, ws, d_out, d_in, "W"))
+    if h is None:
+        h = torch.empty((N, d_out), dtype=torch.float32, device=xc.device)
+    _call_here("molora_mx_matmul", *args, _dev(h, torch.float32, "h", (N, d_out)), N, d_in, d_out, _stream(stream))
+    return h
+
+
+def _bytes(fn, *sizes):
+    return int(getattr(load(), fn)(*sizes))
+
+
+def molora_apply_mx(x, wc, ws, A, B, r, h=None, workspace=None, stream=None):
+    """molora_apply on a base weight in 4-bit blocks: h[i] = Q(x[i]) Q(W) + (x[i] A[r[i]]) B[r[i]]."""
+    N, d_in = _two(x, "x")
+    C, _, rank = _three(A, "A")
+    d_out = _three(B, "B")[2]
+    if h is None:
+        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+    if workspace is None:
+        nbytes = _bytes("molora_apply_mx_workspace_bytes", N, d_in, d_out, C, rank)
+        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=x.device)
+    bf = torch.bfloat16
+    work, work_bytes = _flat_bytes(workspace, "workspace")
+    _call_here("molora_apply_mx", _dev(x, bf, "x"), *_mx(wc, ws, d_out, d_in, "W"), _dev(A, bf, "A", (C, d_in, rank)),
+          _dev(B, bf, "B", (C, rank, d_out)), _dev(r, torch.int32, "r", (N,)), _dev(h, torch.float32, "h", (N, d_out)),
+          N, d_in, d_out, C, rank, work, work_bytes, _stream(stream))
+    return h
+
+
+_ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _gated_args(x, W, A, B, r, act):
+    """(operands for _call, sizes, code of the activation) of the gated block."""
+    N, d_in = _two(x, "x")
+    wide = _two(W, "W")[1]
+    if wide % 2 != 0:
+        raise ValueError(f"W holds a gate and an up half of the same width, not {wide} columns")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {', '.join(_ACTS)}, got {act!r}")
+    given = [t is not None for t in (A, B, r)]
+    if any(given) and not all(given):
+        raise ValueError("A, B and r are given together, or none of them")
+    C, _, rank = _three(A, "A") if A is not None else (0, 0, 0)
+    bf = torch.bfloat16
+    ops = [_dev(x, bf, "x"), _dev(W, bf, "W", (d_in, wide)), _opt(A, bf, "A", (C, d_in, rank)), _opt(B, bf, "B", (C, rank, wide)),
+           _opt(r, torch.int32, "r", (N,))]
+    return ops, (N, d_in, wide // 2, C, rank), _ACTS[act]
+
+
+def _gated_workspace(fn, sizes, workspace, device):
+    if workspace is None:
+        workspace = torch.empty(max(_bytes(fn, *sizes), 256), dtype=torch.uint8, device=device)
+    return _flat_bytes(workspace, "workspace")
+
+
+def molora_apply_gated(x, W, A=None, B=None, r=None, act="silu", z=None, pre=None, workspace=None, stream=None):
+    """z = act(h[:, :F]) * h[:, F:] (bf16 [N][F]) with h = x W + (x A[r]) B[r] of 2 F columns, gate and
+    up side by side.  pre (fp32 [N][2 F]): filled with h, which molora_gated_backward takes.  act: "silu",
+    "gelu" or "gelu_tanh".  Without A, B and r there are no adapters."""
+    ops, sizes, code = _gated_args(x, W, A, B, r, act)
+    N, F = sizes[0], sizes[2]
+    if z is None:
+        z = torch.empty((N, F), dtype=torch.bfloat16, device=x.device)
+    work, work_bytes = _gated_workspace("molora_apply_gated_workspace_bytes", sizes, workspace, x.device)
+    _call_here("molora_apply_gated", *ops, _dev(z, torch.bfloat16, "z", (N, F)), _opt(pre, torch.float32, "pre", (N, 2 * F)), *sizes, code,
+          work, work_bytes, _stream(stream))
+    return z
+
+
+def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A", "B"), dx=None, dW=None, dA=None, dB=None,
+                          workspace=None, stream=None):
+    """The gradients (dx, dW, dA, dB) of molora_apply_gated, bf16, given dz and the pre that it filled.  need:
+    which of them (the others, and dA and dB without adapters, are None)."""
+    ops, sizes, code = _gated_args(x, W, A, B, r, act)
+    N, d_in, F, C, rank = sizes
+    bf = torch.bfloat16
+    unknown = set(need) - {"x", "W", "A", "B"}
+    if unknown:
+        raise ValueError(f"need names x, W, A, B: got {', '.join(sorted(map(str, unknown)))}")
+    out = []
+    for name, t, shape in (("x", dx, (N, d_in)), ("W", dW, (d_in, 2 * F)), ("A", dA, (C, d_in, rank)), ("B", dB, (C, rank, 2 * F))):
+        if name not in need or (C == 0 and name in "AB"):
+            if t is not None:
+                raise ValueError(f"d{name} is given but not needed")
+            out.append((None, None))
+            continue
+        if t is None:
+            t = torch.empty(shape, dtype=bf, device=x.device)
+        out.append((t, _dev(t, bf, f"d{name}", shape)))
+    work, work_bytes = _gated_workspace("molora_gated_backward_workspace_bytes", sizes, workspace, x.device)
+    _call_here("molora_gated_backward", _dev(dz, bf, "dz", (N, F)), *ops, _dev(pre, torch.float32, "pre", (N, 2 * F)), *(d for _, d in out),
+          *sizes, code, work, work_bytes, _stream(stream))
+    return tuple(t for t, _ in out)
 
 
 class Graph:

@@ -1,6 +1,7 @@
 // C ABI of libmolora: argument checking and the order of launches.  No arithmetic here.
 #include "../../include/molora.h"
 
+#include "api_util.h"
 #include "common.h"
 
 #include <mutex>
@@ -75,16 +76,6 @@ void *static_scratch_of_current_device() {
 
 namespace {
 
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned256(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
-inline size_t round256(size_t b) { return (b + 255u) & ~size_t(255); }
-
-inline bool apply_sizes_ok(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank) {
-    return N >= 0 && N < (int64_t(1) << 31) && d_in >= 8 && d_in % 8 == 0 && d_out >= 8 &&
-           d_out % 8 == 0 && C >= 1 && C <= MOLORA_MAX_TARGETS && rank >= 8 && rank % 8 == 0 &&
-           rank <= MOLORA_MAX_RANK;
-}
-
 struct Workspace {
     int32_t *offsets;
     int32_t *perm;
@@ -142,8 +133,6 @@ inline size_t workspace_up_to(int64_t N, int32_t d_in, int32_t d_out, int32_t C,
     if (ks > 1 && N > 0) take(carve(nullptr, small, d_in, d_out, C, rank).bytes + round256(size_t(ks - 1) * size_t(small) * size_t(d_out) * sizeof(float)));
     return most;
 }
-
-inline molora_status from_hip(hipError_t e) { return e == hipSuccess ? MOLORA_OK : MOLORA_EHIP; }
 
 molora_status apply_common(const void *x, const void *W, const void *A, const void *B,
                            const int32_t *r, const int32_t *offsets, const int32_t *perm, float *h,

@@ -1,0 +1,300 @@
+// C ABI of the feed-forward block: 4-bit microscaled products and the gated block.  Argument checking and the
+// order of launches, no arithmetic.
+#include "api_util.h"
+#include "mx.h"
+
+namespace {
+
+// Rows and k of a microscaled operand.
+inline bool mx_sizes_ok(int64_t rows, int32_t K) {
+    return rows >= 0 && rows < (int64_t(1) << 31) && K >= 8 && K % 8 == 0 &&
+           molora::mx_row_tiles(rows) * molora::mx_k_tiles(K) < molora::kMxMaxBlocks;
+}
+inline size_t mx_codes(int64_t rows, int32_t K) {
+    return size_t(molora::mx_row_tiles(rows)) * size_t(molora::mx_k_tiles(K)) * 1024;
+}
+inline size_t mx_scales(int64_t rows, int32_t K) {
+    return size_t(molora::mx_row_tiles(rows)) * size_t(molora::mx_k_groups(K)) * 256;
+}
+inline bool mx_product_ok(int64_t N, int32_t d_in, int32_t d_out) {
+    return d_out >= 8 && d_out % 8 == 0 && mx_sizes_ok(N, d_in) && mx_sizes_ok(d_out, d_in) &&
+           ((N + 127) / 128) * ((int64_t(d_out) + 127) / 128) < molora::kMxMaxBlocks;
+}
+
+struct Cutter {  // pieces of a workspace, each 256-byte aligned
+    unsigned char *base;
+    size_t at = 0;
+    template <class T>
+    T *take(size_t bytes) {
+        T *p = reinterpret_cast<T *>(base + at);
+        at += round256(bytes);
+        return p;
+    }
+};
+
+// ---- routed projection on a microscaled base weight ----
+struct MxWorkspace {
+    int32_t *offsets, *perm;
+    uint16_t *t2;
+    uint8_t *codes, *scales;
+    size_t bytes;
+};
+inline MxWorkspace carve_mx(void *base, int64_t N, int32_t d_in, int32_t C, int32_t rank) {
+    Cutter c{static_cast<unsigned char *>(base)};
+    MxWorkspace w;
+    w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
+    w.perm = c.take<int32_t>(size_t(N) * 4);
+    w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+    w.codes = c.take<uint8_t>(mx_codes(N, d_in));
+    w.scales = c.take<uint8_t>(mx_scales(N, d_in));
+    w.bytes = c.at;
+    return w;
+}
+
+// ---- gated block ----
+inline bool gated_sizes_ok(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t act) {
+    if (act < MOLORA_ACT_SILU || act > MOLORA_ACT_GELU_TANH || F < 8 || F % 8 != 0 || F > (1 << 29)) return false;
+    const bool bare = C == 0 && rank == 0;
+    if (!apply_sizes_ok(N, d_in, 2 * F, bare ? 1 : C, bare ? 8 : rank)) return false;
+    // the tiled kernel's 32-bit offsets into x and W, also as operands of the backward pass
+    return molora::fused_gemm_sizes_ok(N + 7, d_in, 2 * F, 256) && molora::fused_gemm_sizes_ok(N + 7, 2 * F, 8, 256);
+}
+inline bool adapters_given(const void *A, const void *B, const int32_t *r, int32_t C) {
+    return C == 0 ? !A && !B && !r : A && B && r;
+}
+
+constexpr int64_t kGatedStream = 64;  // batches whose projection streams W: molora_apply, then the activation
+
+struct GatedWorkspace {
+    void *apply;  // molora_apply's own
+    size_t apply_bytes;
+    float *pre;
+    int32_t *offsets, *perm;
+    uint16_t *t2;
+    size_t bytes;
+};
+inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
+    Cutter c{static_cast<unsigned char *>(base)};
+    GatedWorkspace w{};
+    if (C > 0 && N <= kGatedStream) {
+        w.apply_bytes = molora_apply_workspace_bytes(N, d_in, 2 * F, C, rank);
+        w.apply = c.take<void>(w.apply_bytes);
+        w.pre = c.take<float>(size_t(N) * 2 * F * 4);
+    } else if (C > 0) {
+        w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
+        w.perm = c.take<int32_t>(size_t(N) * 4);
+        w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+    }
+    w.bytes = c.at;
+    return w;
+}
+
+struct BackwardWorkspace {
+    int32_t *offsets, *perm;
+    uint16_t *t2, *s2, *dh, *xt, *wt, *at, *bt;
+    size_t bytes;
+};
+inline int64_t padded_rows(int64_t N) { return (N + 7) & ~int64_t(7); }
+inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
+    Cutter c{static_cast<unsigned char *>(base)};
+    BackwardWorkspace w{};
+    if (C > 0) {
+        w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
+        w.perm = c.take<int32_t>(size_t(N) * 4);
+        w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+        w.s2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+        w.at = c.take<uint16_t>(size_t(C) * rank * d_in * 2);
+        w.bt = c.take<uint16_t>(size_t(C) * rank * 2 * F * 2);
+    }
+    w.dh = c.take<uint16_t>(size_t(padded_rows(N)) * 2 * F * 2);
+    w.xt = c.take<uint16_t>(size_t(padded_rows(N)) * d_in * 2);
+    w.wt = c.take<uint16_t>(size_t(d_in) * 2 * F * 2);
+    w.bytes = c.at;
+    return w;
+}
+
+#define MOLORA_TRY(call) \
+    if ((call) != hipSuccess) return MOLORA_EHIP
+
+}  // namespace
+
+extern "C" {
+
+size_t molora_mx_codes_bytes(int64_t rows, int32_t K) { return mx_sizes_ok(rows, K) ? mx_codes(rows, K) : 0; }
+size_t molora_mx_scales_bytes(int64_t rows, int32_t K) { return mx_sizes_ok(rows, K) ? mx_scales(rows, K) : 0; }
+
+molora_status molora_mx_quantize(const void *src, int32_t src_type, void *codes, void *scales, int64_t rows, int32_t K,
+                                 void *stream) {
+    if (!mx_sizes_ok(rows, K) || (src_type != MOLORA_BF16 && src_type != MOLORA_F32)) return MOLORA_EINVAL;
+    if (rows == 0) return MOLORA_OK;
+    if (!src || !codes || !scales) return MOLORA_EINVAL;
+    if (!aligned16(src) || !aligned16(codes) || !aligned16(scales)) return MOLORA_EALIGN;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    return from_hip(molora::launch_mx_quantize(src, src_type == MOLORA_F32, nullptr, static_cast<uint8_t *>(codes),
+                                               static_cast<uint8_t *>(scales), rows, K, static_cast<hipStream_t>(stream)));
+}
+
+molora_status molora_mx_quantize_w(const void *W, void *codes, void *scales, int32_t d_in, int32_t d_out, void *stream) {
+    if (d_out < 8 || d_out % 8 != 0 || !mx_sizes_ok(d_out, d_in)) return MOLORA_EINVAL;
+    if (!W || !codes || !scales) return MOLORA_EINVAL;
+    if (!aligned16(W) || !aligned16(codes) || !aligned16(scales)) return MOLORA_EALIGN;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    return from_hip(molora::launch_mx_quantize_w(static_cast<const uint16_t *>(W), static_cast<uint8_t *>(codes),
+                                                 static_cast<uint8_t *>(scales), d_in, d_out,
+                                                 static_cast<hipStream_t>(stream)));
+}
+
+molora_status molora_mx_dequantize(const void *codes, const void *scales, float *dst, int64_t rows, int32_t K,
+                                   void *stream) {
+    if (!mx_sizes_ok(rows, K)) return MOLORA_EINVAL;
+    if (rows == 0) return MOLORA_OK;
+    if (!codes || !scales || !dst) return MOLORA_EINVAL;
+    if (!aligned16(codes) || !aligned16(scales) || !aligned16(dst)) return MOLORA_EALIGN;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    return from_hip(molora::launch_mx_dequantize(static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales),
+                                                 dst, rows, K, static_cast<hipStream_t>(stream)));
+}
+
+molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, const void *ws, float *h, int64_t N,
+                               int32_t d_in, int32_t d_out, void *stream) {
+    if (!mx_product_ok(N, d_in, d_out)) return MOLORA_EINVAL;
+    if (N == 0) return MOLORA_OK;
+    if (!xc || !xs || !wc || !ws || !h) return MOLORA_EINVAL;
+    if (!aligned16(xc) || !aligned16(xs) || !aligned16(wc) || !aligned16(ws) || !aligned16(h)) return MOLORA_EALIGN;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    return from_hip(molora::launch_mx_gemm(static_cast<const uint8_t *>(xc), static_cast<const uint8_t *>(xs),
+                                           static_cast<const uint8_t *>(wc), static_cast<const uint8_t *>(ws), nullptr,
+                                           nullptr, nullptr, nullptr, h, N, d_in, d_out, 0, 0,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank) {
+    if (!apply_sizes_ok(N, d_in, d_out, C, rank) || !mx_product_ok(N, d_in, d_out)) return 0;
+    return carve_mx(nullptr, N, d_in, C, rank).bytes;
+}
+
+molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, const void *A, const void *B, const int32_t *r,
+                              float *h, int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    if (!apply_sizes_ok(N, d_in, d_out, C, rank) || !mx_product_ok(N, d_in, d_out)) return MOLORA_EINVAL;
+    if (N == 0) return MOLORA_OK;
+    if (!x || !wc || !ws || !A || !B || !r || !h || !workspace) return MOLORA_EINVAL;
+    if (!aligned16(x) || !aligned16(wc) || !aligned16(ws) || !aligned16(A) || !aligned16(B) || !aligned16(r) ||
+        !aligned16(h) || !aligned256(workspace))
+        return MOLORA_EALIGN;
+    const MxWorkspace w = carve_mx(workspace, N, d_in, C, rank);
+    if (workspace_bytes < w.bytes) return MOLORA_EWORKSPACE;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint16_t *xb = static_cast<const uint16_t *>(x), *Ab = static_cast<const uint16_t *>(A);
+    const molora::Mix plain{1, C, nullptr, nullptr};
+    MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
+    MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
+    const bool stream_w = N <= 64;  // one read of the codes in token order, then the expand on top
+    MOLORA_TRY(molora::launch_mx_quantize(x, false, stream_w ? nullptr : w.perm, w.codes, w.scales, N, d_in, s));
+    if (stream_w) {
+        MOLORA_TRY(molora::launch_mx_gemm(w.codes, w.scales, static_cast<const uint8_t *>(wc),
+                                          static_cast<const uint8_t *>(ws), nullptr, nullptr, nullptr, nullptr, h, N, d_in,
+                                          d_out, 0, 0, s));
+        return from_hip(molora::launch_small_expand(static_cast<const uint16_t *>(B), w.t2, w.offsets, w.perm, h, N, d_in,
+                                                    d_out, C, rank, plain, s));
+    }
+    return from_hip(molora::launch_mx_gemm(w.codes, w.scales, static_cast<const uint8_t *>(wc),
+                                           static_cast<const uint8_t *>(ws), static_cast<const uint16_t *>(B), w.t2,
+                                           w.offsets, w.perm, h, N, d_in, d_out, C, rank, s));
+}
+
+size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
+    if (!gated_sizes_ok(N, d_in, F, C, rank, 0)) return 0;
+    const size_t a = carve_gated(nullptr, N, d_in, F, C, rank).bytes;
+    const size_t b = carve_gated(nullptr, N < kGatedStream ? N : kGatedStream, d_in, F, C, rank).bytes;
+    return a > b ? a : b;
+}
+
+molora_status molora_apply_gated(const void *x, const void *W, const void *A, const void *B, const int32_t *r, void *z,
+                                 float *pre, int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t act,
+                                 void *workspace, size_t workspace_bytes, void *stream) {
+    if (!gated_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
+    if (N == 0) return MOLORA_OK;
+    if (!x || !W || !z || !adapters_given(A, B, r, C) || (C > 0 && !workspace)) return MOLORA_EINVAL;
+    if (!aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(r) || !aligned16(z) ||
+        !aligned16(pre) || !aligned256(workspace))
+        return MOLORA_EALIGN;
+    const GatedWorkspace w = carve_gated(workspace, N, d_in, F, C, rank);
+    if (workspace_bytes < w.bytes) return MOLORA_EWORKSPACE;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint16_t *zb = static_cast<uint16_t *>(z);
+    const uint16_t *xb = static_cast<const uint16_t *>(x), *Wb = static_cast<const uint16_t *>(W);
+    const uint16_t *Ab = static_cast<const uint16_t *>(A), *Bb = static_cast<const uint16_t *>(B);
+    if (C > 0 && N <= kGatedStream) {
+        float *h = pre != nullptr ? pre : w.pre;
+        const molora_status st = molora_apply(x, W, A, B, r, h, N, d_in, 2 * F, C, rank, w.apply, w.apply_bytes, stream);
+        return st != MOLORA_OK ? st : from_hip(molora::launch_gate(h, zb, N, F, act, s));
+    }
+    if (C > 0) {
+        MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
+        MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank,
+                                         molora::Mix{1, C, nullptr, nullptr}, s));
+    }
+    return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, N, d_in, F, C, rank, act, s));
+}
+
+size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
+    return gated_sizes_ok(N, d_in, F, C, rank, 0) ? carve_backward(nullptr, N, d_in, F, C, rank).bytes : 0;
+}
+
+molora_status molora_gated_backward(const void *dz, const void *x, const void *W, const void *A, const void *B,
+                                    const int32_t *r, const float *pre, void *dx, void *dW, void *dA, void *dB, int64_t N,
+                                    int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t act, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+    if (!gated_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
+    if (C == 0 && (dA || dB)) return MOLORA_EINVAL;
+    if (N == 0) {  // sums over no tokens
+        if (!aligned16(dW) || !aligned16(dA) || !aligned16(dB)) return MOLORA_EALIGN;
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        if (dW) MOLORA_TRY(molora::launch_zero(dW, int64_t(d_in) * F * 4, s));
+        if (dA) MOLORA_TRY(molora::launch_zero(dA, int64_t(C) * d_in * rank * 2, s));
+        if (dB) MOLORA_TRY(molora::launch_zero(dB, int64_t(C) * rank * F * 4, s));
+        return MOLORA_OK;
+    }
+    if (!dz || !x || !W || !pre || !adapters_given(A, B, r, C) || !workspace) return MOLORA_EINVAL;
+    if (!aligned16(dz) || !aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(r) ||
+        !aligned16(pre) || !aligned16(dx) || !aligned16(dW) || !aligned16(dA) || !aligned16(dB) || !aligned256(workspace))
+        return MOLORA_EALIGN;
+    const BackwardWorkspace w = carve_backward(workspace, N, d_in, F, C, rank);
+    if (workspace_bytes < w.bytes) return MOLORA_EWORKSPACE;
+    if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint16_t *xb = static_cast<const uint16_t *>(x), *Wb = static_cast<const uint16_t *>(W);
+    const uint16_t *Ab = static_cast<const uint16_t *>(A), *Bb = static_cast<const uint16_t *>(B);
+    const molora::Mix plain{1, C, nullptr, nullptr};
+    const int64_t Np = padded_rows(N);
+    MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
+    if (C > 0) {
+        MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
+        if (dx || dA) {  // s = dh B^T
+            MOLORA_TRY(molora::launch_transpose(Bb, w.bt, C, rank, 2 * F, rank, s));
+            MOLORA_TRY(molora::launch_shrink(w.dh, w.bt, w.offsets, w.perm, w.s2, N, 2 * F, C, rank, plain, s));
+        }
+        if (dB) MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
+        if (dA)
+            MOLORA_TRY(molora::launch_grouped_outer(xb, w.s2, w.offsets, w.perm, static_cast<uint16_t *>(dA), N, d_in, C, rank, false, s));
+        if (dB)
+            MOLORA_TRY(molora::launch_grouped_outer(w.dh, w.t2, w.offsets, w.perm, static_cast<uint16_t *>(dB), N, 2 * F, C, rank, true, s));
+    }
+    if (dx) {
+        MOLORA_TRY(molora::launch_transpose(Wb, w.wt, 1, d_in, 2 * F, d_in, s));
+        if (C > 0) MOLORA_TRY(molora::launch_transpose(Ab, w.at, C, d_in, rank, d_in, s));
+        MOLORA_TRY(molora::launch_gemm_bf16(w.dh, w.wt, w.at, w.s2, w.offsets, C > 0 ? w.perm : nullptr,
+                                            static_cast<uint16_t *>(dx), N, 2 * F, d_in, C, rank, s));
+    }
+    if (dW) {
+        MOLORA_TRY(molora::launch_transpose(xb, w.xt, 1, N, d_in, Np, s));
+        MOLORA_TRY(molora::launch_gemm_bf16(w.xt, w.dh, nullptr, nullptr, nullptr, nullptr, static_cast<uint16_t *>(dW), d_in,
+                                            (int)Np, 2 * F, 0, 0, s));
+    }
+    return MOLORA_OK;
+}
+
+}  // extern "C"

@@ -181,6 +181,34 @@ hipError_t launch_fused_gemm(const uint16_t *x, const uint16_t *W, const uint16_
 // 0 stages for the streaming kernel
 void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile);
 
+// ---- the fused GEMM with other outputs (gemm_out.hip); offsets, perm and t2 as launch_fused_gemm, or perm == nullptr and
+// C = 0: rows in order, without adapters.  Operands below 4 GiB each (fused_gemm_sizes_ok with a tile forced). ----
+// out = x W + t B_c in bf16
+hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                            const int32_t *offsets, const int32_t *perm, uint16_t *out, int64_t N, int d_in, int d_out,
+                            int C, int rank, hipStream_t s);
+// h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr
+hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                             const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, int64_t N, int d_in,
+                             int F, int C, int rank, int act, hipStream_t s);
+// the tile configuration that the cost rule takes where the streaming kernel is not to be had
+int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
+
+// ---- around the gated block (gated.hip) ----
+hipError_t launch_gate(const float *pre, uint16_t *z, int64_t N, int F, int act, hipStream_t s);
+// dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F]; rows N .. padded - 1 are zero
+hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
+                                int act, hipStream_t s);
+// dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on
+hipError_t launch_transpose(const uint16_t *src, uint16_t *dst, int64_t batch, int64_t rows, int64_t cols, int64_t padded,
+                            hipStream_t s);
+// out[c] = sum over the positions p of bucket c of outer(y[perm[p]], s_p), bf16: [D][R], or [R][D] when flat;
+// y [N][D], s2 [N][2 R] in the layout of the shrink's output.  Empty buckets give zeros.
+hipError_t launch_grouped_outer(const uint16_t *y, const uint16_t *s2, const int32_t *offsets, const int32_t *perm,
+                                uint16_t *out, int64_t N, int D, int C, int R, bool flat, hipStream_t s);
+
+hipError_t launch_zero(void *dst, int64_t bytes, hipStream_t s);  // bytes a multiple of 16
+
 // columns per workgroup of the streaming kernel, 32 or 64
 int small_batch_cols(int64_t N, int d_out);
 // same contract, N <= 64 (the fused GEMM launcher routes such batches here)
