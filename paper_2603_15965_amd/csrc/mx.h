@@ -9,6 +9,7 @@
 // row and block in four k tiles one after the other; the instruction picks the byte.
 // Rows are padded to 16, codes along k to 128 and scales to 512, with zero codes under zero bytes.
 #pragma once
+#include "../../include/molora.h"
 #include "common.h"
 
 namespace molora {

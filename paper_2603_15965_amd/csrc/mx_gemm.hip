@@ -77,23 +77,30 @@ __global__ __launch_bounds__(512) void mx_stream_kernel(const uint8_t *__restric
 }
 
 // ---- larger batches: output tiles ----
-// BM x BN output tile, WM x WN wavefronts.  A stage is 256 k of both sides (two code tiles per 16 rows or
-// columns) brought to LDS as it lies in memory; two stages, one travelling while the other is multiplied.
-// The scales of 512 k come with every second stage, into one of two places of their own.
-template <int WM_, int WN_, int TM_, int TN_>
+// BM x BN output tile, WM x WN wavefronts of TM x TN tiles of 16 x 16.  A stage is 128 k of both sides, brought to
+// LDS as it lies in memory; of three or four stages one is multiplied while the others travel, and a k tile costs one
+// barrier.  The scales of 512 k have one place: a wavefront holds its own in registers for four k tiles, and
+// the next ones are sent for when every wavefront has passed the barrier behind that read.
+// 8192 x 12288 -> 4096: 176 us, 4.7 PFLOP/s.  On random codes the instruction sustains 6.9 from registers and 6.2 with its
+// operands read from LDS at this tile's rate (zeros 9.7 and 8.3: power); without the loads of the loop the kernel takes
+// 161 us.  Reads in front of a k tile's products instead of behind the products before: 204 us; two barriers and
+// stages of 256 k, 258.  With d_in = 4096 the stores of h count: 16384 x 4096 -> 12288 takes 400 us, 805 MB of them.
+template <int WM_, int WN_, int TM_, int TN_, int STAGES_>
 struct MxCfg {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, STAGES = STAGES_;
     static constexpr int NW = WM * WN, NT = NW * 64;
     static constexpr int RT = WM * TM, CT = WN * TN;  // 16-row and 16-column tiles
     static constexpr int BM = RT * 16, BN = CT * 16;
-    static constexpr int PIECES = 2 * (RT + CT), LPW = PIECES / NW;
+    static constexpr int PIECES = RT + CT, LPW = PIECES / NW;
     static constexpr int STAGE = PIECES * 1024;
-    static constexpr int SP = (RT + CT) / 4, SLPW = (SP + NW - 1) / NW;  // 1 KB holds the scales of four tiles
-    static constexpr int SCALES = SP * 1024;
+    static constexpr int SP = PIECES / 4, SLPW = (SP + NW - 1) / NW;  // 1 KB holds the scales of four tiles
     static constexpr int B_STRIDE = BN * 2 + 32;  // a row of B in LDS: four consecutive rows on distinct banks
-    static constexpr size_t LDS_BYTES = 2 * (STAGE + SCALES) + (1024 + 4) * 4;
+    static constexpr int OUT_STRIDE = TN * 64 + 16;  // a row of a wavefront's 16 rows on their way to h
+    static constexpr size_t LDS_BYTES = STAGES * STAGE + SP * 1024;
+    static_assert(STAGES >= 3 && STAGES <= 4, "scales are sent for after their place was read");
     static_assert(PIECES % NW == 0 && RT % 4 == 0 && CT % 4 == 0, "pieces split evenly");
-    static_assert(16 * B_STRIDE <= STAGE, "a slab of B fits a stage");
+    static_assert(16 * B_STRIDE + (MOLORA_MAX_TARGETS + 4) * 4 <= STAGES * STAGE, "a slab of B and the offsets fit the stages");
+    static_assert(NW * 16 * OUT_STRIDE <= STAGES * STAGE, "the epilogue fits the stages");
 };
 
 template <class Cfg>
@@ -102,10 +109,9 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
     const uint8_t *__restrict__ ws, const uint16_t *__restrict__ B, const uint16_t *__restrict__ t2,
     const int32_t *__restrict__ offsets, const int32_t *__restrict__ perm, float *__restrict__ h, int N, int d_out,
     int kt_n, int kg_n, int C, int R, int tiles_m, int tiles_n) {
-    constexpr int TM = Cfg::TM, TN = Cfg::TN, RT = Cfg::RT, CT = Cfg::CT, NW = Cfg::NW;
+    constexpr int TM = Cfg::TM, TN = Cfg::TN, RT = Cfg::RT, NW = Cfg::NW, STAGES = Cfg::STAGES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    unsigned char *const scales = smem + 2 * Cfg::STAGE;
-    int32_t *const off = (int32_t *)(scales + 2 * Cfg::SCALES);
+    unsigned char *const scales = smem + STAGES * Cfg::STAGE;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
@@ -119,32 +125,31 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
     const int tile_m = first + in_group % width, tile_n = in_group / width;
     const int p0 = tile_m * Cfg::BM;
     const int64_t rt_last = (N + 15) / 16 - 1, ct_last = (d_out + 15) / 16 - 1;
-    const int64_t rt0 = (int64_t)tile_m * RT, ct0 = (int64_t)tile_n * CT;
+    const int64_t rt0 = (int64_t)tile_m * RT, ct0 = (int64_t)tile_n * Cfg::CT;
 
-    auto issue = [&](int st) __attribute__((always_inline)) {
-        unsigned char *stage = smem + (st & 1) * Cfg::STAGE;
+    // this wavefront's pieces (rows first, then columns; a tile past the last one: the last one again) at k tile 0
+    const uint8_t *src[Cfg::LPW];
 #pragma unroll
-        for (int i = 0; i < Cfg::LPW; ++i) {
-            const int piece = i * NW + wave;  // [tile][two k tiles], rows first
-            const int kt = min(2 * st + (piece & 1), kt_n - 1);
-            const int tile = piece >> 1;
-            const bool is_x = tile < RT;
-            const int64_t at = is_x ? min(rt0 + tile, rt_last) : min(ct0 + tile - RT, ct_last);
-            load_to_lds16((is_x ? xc : wc) + (at * kt_n + kt) * 1024, lane * 16, stage + piece * 1024);
-        }
-        if (st & 1) return;
-        unsigned char *place = scales + ((st >> 1) & 1) * Cfg::SCALES;
-#pragma unroll
-        for (int i = 0; i < Cfg::SLPW; ++i) {
-            const int piece = (i * NW + wave) % Cfg::SP;  // (twice the same where there are more wavefronts than pieces)
-            const int tile = piece * 4 + (lane >> 4);
-            const bool is_x = piece * 4 < RT;
-            const int64_t at = is_x ? min(rt0 + tile, rt_last) : min(ct0 + tile - RT, ct_last);
-            load_to_lds16_ptr((is_x ? xs : ws) + (at * kg_n + (st >> 1)) * 256 + (lane & 15) * 16, place + piece * 1024);
-        }
+    for (int i = 0; i < Cfg::LPW; ++i) {
+        const int tile = i * NW + wave;
+        const bool is_x = tile < RT;
+        src[i] = (is_x ? xc : wc) + (is_x ? min(rt0 + tile, rt_last) : min(ct0 + tile - RT, ct_last)) * kt_n * 1024;
+    }
+    // piece i of k tile kt, to its stage
+    auto issue_piece = [&](int kt, unsigned char *stage, int i) __attribute__((always_inline)) {
+        load_to_lds16(src[i] + (int64_t)kt * 1024, lane * 16, stage + (i * NW + wave) * 1024);
     };
-
-    for (int i = tid; i <= C && C > 0; i += Cfg::NT) off[i] = offsets[i];
+    const uint8_t *scale_src[Cfg::SLPW];  // this lane's
+#pragma unroll
+    for (int i = 0; i < Cfg::SLPW; ++i) {
+        const int tile = (i * NW + wave) % Cfg::SP * 4 + (lane >> 4);  // (twice the same where there are more wavefronts than pieces)
+        scale_src[i] = (tile < RT ? xs + min(rt0 + tile, rt_last) * kg_n * 256 : ws + min(ct0 + tile - RT, ct_last) * kg_n * 256) + (lane & 15) * 16;
+    }
+    auto issue_scales = [&](int kt) __attribute__((always_inline)) {  // of the four k tiles from kt on
+#pragma unroll
+        for (int i = 0; i < Cfg::SLPW; ++i)
+            load_to_lds16_ptr(scale_src[i] + (int64_t)(kt >> 2) * 256, scales + (i * NW + wave) % Cfg::SP * 1024);
+    };
 
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -152,52 +157,142 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const int nst = (kt_n + 1) / 2;
-    __syncthreads();
-    issue(0);
-    if (nst > 1) issue(1);
-    auto multiply = [&](int st, auto half_c) __attribute__((always_inline)) {
-        constexpr int HALF = decltype(half_c)::value;  // which two bytes of the scales
-        if (st + 1 < nst)
-            wait_vmcnt<Cfg::LPW + (HALF ? Cfg::SLPW : 0)>();  // the next stage may be on its way
-        else
-            wait_vmcnt<0>();
-        wg_barrier();
-        const unsigned char *stage = smem + HALF * Cfg::STAGE;
-        const unsigned char *place = scales + ((st >> 1) & 1) * Cfg::SCALES;
-        uint32_t sx[TM], sw[TN];
+    // A k tile is TM places, one x fragment times the TN of W each.  Behind a place's products the x fragment NA
+    // places ahead is read, and in the last NA places the W fragments of the next k tile.  The workgroup barrier
+    // sits in front of these: there every wavefront holds the last fragments of its k tile, so the stage is
+    // filled again (k tile kt + STAGES) and the first fragments of the next one are read behind products.
+    constexpr int NA = TM < 4 ? TM : 4;
+    static_assert(TM % NA == 0, "a place's fragment is in register set place % NA");
+    u32x4 x[NA], w[2][TN];
+    uint32_t sx[TM], sw[TN], sw_next[TN];
+    const unsigned char *const x_lane = smem + wm * TM * 1024 + lane * 16;
+    const unsigned char *const w_lane = smem + (RT + wn * TN) * 1024 + lane * 16;
+    const unsigned char *const s_lane = scales + lane * 4;
+    auto read_x = [&](int stage, int i) __attribute__((always_inline)) { x[i % NA] = *(const u32x4 *)(x_lane + stage + i * 1024); };
+    auto read_sx = [&](int i) __attribute__((always_inline)) { sx[i] = *(const uint32_t *)(s_lane + (wm * TM + i) * 256); };
+    auto read_sw = [&](int j) __attribute__((always_inline)) { sw_next[j] = *(const uint32_t *)(s_lane + (RT + wn * TN + j) * 256); };
+
 #pragma unroll
-        for (int i = 0; i < TM; ++i) sx[i] = *(const uint32_t *)(place + (wm * TM + i) * 256 + lane * 4);
+    for (int st = 0; st < STAGES; ++st) {
+        if (st >= kt_n) break;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sw[j] = *(const uint32_t *)(place + (RT + wn * TN + j) * 256 + lane * 4);
+        for (int i = 0; i < Cfg::LPW; ++i) issue_piece(st, smem + st * Cfg::STAGE, i);
+        if (st == 0) issue_scales(0);
+    }
+    if (kt_n >= STAGES)
+        wait_vmcnt<(STAGES - 1) * Cfg::LPW>();
+    else
+        wait_vmcnt<0>();
+    wg_barrier();
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (k == 1 && 2 * st + 1 >= kt_n) break;
-            u32x4 w[TN];
+    for (int i = 0; i < NA; ++i) read_x(0, i);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) w[j] = *(const u32x4 *)(stage + ((RT + wn * TN + j) * 2 + k) * 1024 + lane * 16);
+    for (int j = 0; j < TN; ++j) w[0][j] = *(const u32x4 *)(w_lane + j * 1024);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const u32x4 x = *(const u32x4 *)(stage + ((wm * TM + i) * 2 + k) * 1024 + lane * 16);
+    for (int i = 0; i < TM; ++i) read_sx(i);
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = k ? mx_mfma<HALF * 2 + 1>(w[j], x, acc[i][j], sw[j], sx[i])
-                                  : mx_mfma<HALF * 2>(w[j], x, acc[i][j], sw[j], sx[i]);
+    for (int j = 0; j < TN; ++j) {
+        read_sw(j);
+        sw[j] = sw_next[j];
+    }
+
+    int cur = 0;  // the k tile's stage, its offset
+    // J: the k tile's byte of the scales, and the parity of its register set.  Without a branch inside, or the
+    // compiler moves products behind later reads.
+    auto multiply = [&](int kt, auto j_c) __attribute__((always_inline)) {
+        constexpr int J = decltype(j_c)::value, LATE = TM - NA, PER = (Cfg::LPW + NA - 1) / NA;
+        const int nxt = cur == (STAGES - 1) * Cfg::STAGE ? 0 : cur + Cfg::STAGE;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            if (i == LATE) {
+                wait_lds();  // this wavefront has read the stage
+                // its part of the next one is there; those behind it may be on their way
+                wait_vmcnt<(STAGES - 2) * Cfg::LPW + (J == 2 || (STAGES == 4 && J == 1) ? Cfg::SLPW : 0)>();
+                wg_barrier();
+            }
+            if (i >= LATE) {
+#pragma unroll
+                for (int j = i - LATE; j < TN; j += NA) w[(J + 1) & 1][j] = *(const u32x4 *)(w_lane + nxt + j * 1024);
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mx_mfma<J>(w[J & 1][j], x[i % NA], acc[i][j], sw[j], sx[i]);
+            if (i < LATE) {
+                read_x(cur, i + NA);
+            } else {
+                read_x(nxt, i - LATE);
+                if (J == 3) {
+#pragma unroll
+                    for (int k = i % NA; k < TM; k += NA) read_sx(k);
+#pragma unroll
+                    for (int j = i - LATE; j < TN; j += NA) read_sw(j);
+                }
+#pragma unroll
+                for (int u = (i - LATE) * PER; u < (i - LATE + 1) * PER && u < Cfg::LPW; ++u) issue_piece(kt + STAGES, smem + cur, u);
+                if ((J + STAGES) % 4 == 0 && i == TM - 1) issue_scales(kt + STAGES);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (J == 3) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) sw[j] = sw_next[j];
+        }
+        cur = nxt;
+    };
+    int kt = 0;
+    for (; kt + 3 + STAGES < kt_n; kt += 4) {
+        multiply(kt, std::integral_constant<int, 0>{});
+        multiply(kt + 1, std::integral_constant<int, 1>{});
+        multiply(kt + 2, std::integral_constant<int, 2>{});
+        multiply(kt + 3, std::integral_constant<int, 3>{});
+    }
+    // the last k tiles, at most STAGES + 3, one at a time; kt is a multiple of four, stage cur is there
+    for (const int kt0 = kt; kt < kt_n; ++kt) {
+        if (kt != kt0) {
+            const int before = cur;
+            cur = cur == (STAGES - 1) * Cfg::STAGE ? 0 : cur + Cfg::STAGE;
+            wait_lds();
+            if (kt + STAGES - 2 < kt_n)
+                wait_vmcnt<(STAGES - 2) * Cfg::LPW>();
+            else
+                wait_vmcnt<0>();
+            wg_barrier();
+            if (const int next = kt - 1 + STAGES; next < kt_n) {
+#pragma unroll
+                for (int i = 0; i < Cfg::LPW; ++i) issue_piece(next, smem + before, i);
+                if (next % 4 == 0) issue_scales(next);
+            }
+            if (kt % 4 == 0) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) read_sx(i);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    read_sw(j);
+                    sw[j] = sw_next[j];
+                }
             }
         }
-        wait_lds();
-        wg_barrier();  // every wavefront has read the stage: it can be filled again
-        if (st + 2 < nst) issue(st + 2);
-    };
-    for (int st = 0; st < nst; st += 2) {
-        multiply(st, std::integral_constant<int, 0>{});
-        if (st + 1 < nst) multiply(st + 1, std::integral_constant<int, 1>{});
+        u32x4 wt[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) wt[j] = *(const u32x4 *)(w_lane + cur + j * 1024);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const u32x4 xt = *(const u32x4 *)(x_lane + cur + i * 1024);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mx_mfma<0>(wt[j], xt, acc[i][j], sw[j], sx[i]);
+            sx[i] >>= 8;
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sw[j] >>= 8;
     }
+    __syncthreads();  // the stages are free
 
     // ---- expand: the buckets that own rows of the tile, 16 columns of t at a time ----
     // A fragment of 32 k is [hi | lo] of 16 columns of t against the same 16 rows of B twice.
     const int kq = lane >> 4, l16 = lane & 15;
     if (C > 0) {
+        int32_t *const off = (int32_t *)(smem + 16 * Cfg::B_STRIDE);
+        for (int i = tid; i <= C; i += Cfg::NT) off[i] = offsets[i];
+        __syncthreads();
         int lo_c = 0, hi_c = C;  // first bucket that ends behind the tile's first row
         while (lo_c < hi_c) {
             const int mid = (lo_c + hi_c) >> 1;
@@ -237,17 +332,26 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
                 }
             }
         }
+        __syncthreads();
     }
 
+    // ---- epilogue: 16 rows at a time through a region of the wavefront's own, so that a store instruction
+    // covers TN * 64 contiguous bytes of each of its rows ----
+    unsigned char *const own = smem + wave * (16 * Cfg::OUT_STRIDE);
+    constexpr int LPR = TN * 4, RPI = 64 / LPR;  // lanes to a row, rows to an instruction
+    const int64_t col = (ct0 + wn * TN) * 16 + lane % LPR * 4;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int p = p0 + (wm * TM + i) * 16 + l16;
-        if (p >= N) continue;
-        const int64_t row = perm != nullptr ? perm[p] : p;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t col = (ct0 + wn * TN + j) * 16 + kq * 4;
-            if (col < d_out) __builtin_nontemporal_store(acc[i][j], (f32x4 *)(h + row * d_out + col));
+        for (int j = 0; j < TN; ++j) *(f32x4 *)(own + l16 * Cfg::OUT_STRIDE + j * 64 + kq * 16) = acc[i][j];
+#pragma unroll
+        for (int k = 0; k < 16 / RPI; ++k) {
+            const int in = k * RPI + lane / LPR, p = p0 + (wm * TM + i) * 16 + in;
+            const f32x4 v = *(const f32x4 *)(own + in * Cfg::OUT_STRIDE + lane % LPR * 16);
+            if (p < N && col < d_out) {
+                const int64_t row = perm != nullptr ? perm[p] : p;
+                __builtin_nontemporal_store(v, (f32x4 *)(h + row * d_out + col));
+            }
         }
     }
 }
@@ -272,8 +376,44 @@ hipError_t launch_mx_tiles(const uint8_t *xc, const uint8_t *xs, const uint8_t *
 
 }  // namespace
 
-using MxBig = MxCfg<2, 4, 8, 4>;    // 256 x 256, one workgroup per compute unit
-using MxSmall = MxCfg<2, 2, 4, 4>;  // 128 x 128, two
+using Mx256 = MxCfg<2, 4, 8, 4, 4>;   // 256 x 256, one workgroup per compute unit
+using MxWide = MxCfg<2, 2, 8, 4, 3>;  // 256 x 128, two
+using Mx128 = MxCfg<2, 2, 4, 4, 3>;   // 128 x 128, three
+using MxLow = MxCfg<1, 4, 4, 2, 4>;   // 64 x 128, four
+using Mx64 = MxCfg<2, 2, 2, 2, 4>;    // 64 x 64, five
+
+namespace {
+// The tile from the sizes: the least of the costs below (us).  Tiles run in rounds of 256 compute units x workgroups per
+// unit; a whole round costs a start and an end and a time per k tile of 128, the last one parts of both that
+// grow with its share of the places.  Coefficients: non-negative least squares of the relative error over 96
+// shapes, 65 .. 16384 rows, 256 .. 12288 deep, 1024 .. 12288 wide, every configuration timed on each.  The choice is
+// 2 % behind the best configuration there (geometric mean), the large tiles alone 60 %, the smallest alone 35 %.
+struct MxCost {
+    int bm, bn, per_cu;
+    double once, round, part, last, k_round, k_part, k_last;
+};
+constexpr MxCost kMxCosts[] = {
+    {256, 256, 1, 3.8, 11.4, 4.3, 1.4, 0.784, 0.512, 0.314}, {256, 128, 2, 7.7, 9.4, 0.0, 2.3, 0.755, 0.316, 0.331},
+    {128, 128, 3, 3.3, 6.8, 1.7, 4.3, 0.598, 0.217, 0.263},  {64, 128, 4, 3.8, 4.3, 0.1, 2.8, 0.561, 0.119, 0.309},
+    {64, 64, 5, 3.2, 2.7, 0.0, 2.0, 0.444, 0.091, 0.291}};
+
+int mx_tile_choice(int64_t N, int d_in, int d_out) {
+    const double kt = mx_k_tiles(d_in);
+    double best = 1e30;
+    int pick = 0;
+    for (int i = 0; i < 5; ++i) {
+        const MxCost &c = kMxCosts[i];
+        const int64_t tiles = ((N + c.bm - 1) / c.bm) * (((int64_t)d_out + c.bn - 1) / c.bn), slots = 256 * c.per_cu;
+        const double full = (double)(tiles / slots), last = (double)(tiles % slots) / (double)slots, part = last > 0 ? 1 : 0;
+        const double cost = c.once + full * (c.round + kt * c.k_round) + part * (c.part + kt * c.k_part) + last * (c.last + kt * c.k_last);
+        if (cost < best) {
+            best = cost;
+            pick = i;
+        }
+    }
+    return pick;
+}
+}  // namespace
 
 hipError_t launch_mx_gemm(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, const uint8_t *ws, const uint16_t *B,
                           const uint16_t *t2, const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in,
@@ -290,9 +430,15 @@ hipError_t launch_mx_gemm(const uint8_t *xc, const uint8_t *xs, const uint8_t *w
 #undef MOLORA_MX_STREAM
         return hipGetLastError();
     }
-    const int64_t big = ((N + 255) / 256) * (((int64_t)d_out + 255) / 256);
-    if (big >= 256) return launch_mx_tiles<MxBig>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, s);
-    return launch_mx_tiles<MxSmall>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, s);
+#define MOLORA_MX_TILES(CFG) launch_mx_tiles<CFG>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, s)
+    switch (mx_tile_choice(N, d_in, d_out)) {  // the order of kMxCosts
+        case 0: return MOLORA_MX_TILES(Mx256);
+        case 1: return MOLORA_MX_TILES(MxWide);
+        case 2: return MOLORA_MX_TILES(Mx128);
+        case 3: return MOLORA_MX_TILES(MxLow);
+        default: return MOLORA_MX_TILES(Mx64);
+    }
+#undef MOLORA_MX_TILES
 }
 
 }  // namespace molora
