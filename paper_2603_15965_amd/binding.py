@@ -5,6 +5,7 @@ step of the path runs in the library's kernels.  There is no fallback: if the li
 not built, the first call raises.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -702,15 +703,27 @@ def molora_apply_mix(x, W, A, B, idx, w=None, slots=None, C=None, h=None, worksp
 
 def _call_here(fn, *args):
     """_call for the operators below, whose launches go to the current device: tensors of another one are
-    refused (their addresses mean nothing there)."""
-    if _raw_device is not None and torch.cuda.is_initialized():
-        here = _raw_device()
-        for a in args:
-            if type(a) is tuple and isinstance(a[0], _Tensor) and a[0].is_cuda and a[0].get_device() != here:
-                raise ValueError(f"{a[2]} is on cuda:{a[0].get_device()}, the current device is cuda:{here}")
-    _call(fn, *args)
+    refused (their addresses mean nothing there).  One pass over the arguments, which a small batch waits for."""
+    here = _raw_device() if _raw_device is not None and torch.cuda.is_initialized() else None
+    raw = []
+    for a in args:
+        if type(a) is tuple:
+            t, dtype, name, shape = a
+            if not (isinstance(t, _Tensor) and t.dtype is dtype and (shape is None or t.shape == shape) and t.is_contiguous()
+                    and (t.is_cuda if here is None else t.get_device() == here)):
+                _complain(args)
+                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+            raw.append(t.data_ptr())
+        elif type(a) is _S:
+            raw.append(_stream_now(a.stream))
+        else:
+            raw.append(a)
+    st = getattr(_lib or load(), fn)(*raw)
+    if st != MOLORA_OK:
+        raise MoloraError(st, fn)
 
 
+@functools.lru_cache(maxsize=512)
 def _mx_shapes(rows, K):
     """Shapes of the codes and scales of a microscaled operand."""
     if rows < 0 or K < 8 or K % 8 != 0:
@@ -719,12 +732,12 @@ def _mx_shapes(rows, K):
     return (tiles, -(-K // 128), 64, 16), (tiles, -(-K // 512), 64, 4)
 
 
-def _mx_outputs(rows, K, codes, scales, device):
+def _mx_outputs(rows, K, codes, scales, like):
     c, s = _mx_shapes(rows, K)
     if codes is None:
-        codes = torch.empty(c, dtype=torch.uint8, device=device)
+        codes = like.new_empty(c, dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty(s, dtype=torch.uint8, device=device)
+        scales = like.new_empty(s, dtype=torch.uint8)
     return codes, scales
 
 
@@ -738,7 +751,7 @@ def molora_mx_quantize(x, codes=None, scales=None, stream=None):
     rows, K = _two(x, "x")
     if x.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"x must be bfloat16 or float32, got {x.dtype}")
-    codes, scales = _mx_outputs(rows, K, codes, scales, x.device)
+    codes, scales = _mx_outputs(rows, K, codes, scales, x)
     _call_here("molora_mx_quantize", _dev(x, x.dtype, "x"), int(x.dtype is torch.float32), *_mx(codes, scales, rows, K, "x"), rows, K,
           _stream(stream))
     return codes, scales
@@ -747,7 +760,7 @@ def molora_mx_quantize(x, codes=None, scales=None, stream=None):
 def molora_mx_quantize_w(W, codes=None, scales=None, stream=None):
     """A base weight W [d_in][d_out] (bf16) to 4-bit blocks along d_in: (codes, scales), done once."""
     d_in, d_out = _two(W, "W")
-    codes, scales = _mx_outputs(d_out, d_in, codes, scales, W.device)
+    codes, scales = _mx_outputs(d_out, d_in, codes, scales, W)
     _call_here("molora_mx_quantize_w", _dev(W, torch.bfloat16, "W"), *_mx(codes, scales, d_out, d_in, "W"), d_in, d_out, _stream(stream))
     return codes, scales
 
@@ -757,7 +770,7 @@ def molora_mx_dequantize(codes, scales, rows, K, out=None, stream=None):
     rows, K = int(rows), int(K)
     args = _mx(codes, scales, rows, K, "operand")
     if out is None:
-        out = torch.empty((rows, K), dtype=torch.float32, device=codes.device)
+        out = codes.new_empty((rows, K), dtype=torch.float32)
     _call_here("molora_mx_dequantize", *args, _dev(out, torch.float32, "out", (rows, K)), rows, K, _stream(stream))
     return out
 
@@ -767,7 +780,7 @@ def molora_mx_matmul(xc, xs, wc, ws, N, d_in, d_out, h=None, stream=None):
     N, d_in, d_out = int(N), int(d_in), int(d_out)
     args = (*_mx(xc, xs, N, d_in, "x"), *_mx(wc, ws, d_out, d_in, "W"))
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=xc.device)
+        h = xc.new_empty((N, d_out), dtype=torch.float32)
     _call_here("molora_mx_matmul", *args, _dev(h, torch.float32, "h", (N, d_out)), N, d_in, d_out, _stream(stream))
     return h
 

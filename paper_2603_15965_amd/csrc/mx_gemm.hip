@@ -99,7 +99,7 @@ struct MxCfg {
     static constexpr size_t LDS_BYTES = STAGES * STAGE + SP * 1024;
     static_assert(STAGES >= 3 && STAGES <= 4, "scales are sent for after their place was read");
     static_assert(PIECES % NW == 0 && RT % 4 == 0 && CT % 4 == 0, "pieces split evenly");
-    static_assert(16 * B_STRIDE + (MOLORA_MAX_TARGETS + 4) * 4 <= STAGES * STAGE, "a slab of B and the offsets fit the stages");
+    static_assert(2 * 32 * B_STRIDE <= STAGES * STAGE, "two slabs of B fit the stages");
     static_assert(NW * 16 * OUT_STRIDE <= STAGES * STAGE, "the epilogue fits the stages");
 };
 
@@ -196,6 +196,19 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
         sw[j] = sw_next[j];
     }
 
+    // the first bucket that ends behind the tile's first row
+    int c_first = C, lo_first = 0, hi_first = 0;
+    for (int c0 = 0; c0 < C; c0 += 64) {
+        const int end = offsets[min(c0 + lane, C - 1) + 1];
+        const uint64_t behind = __ballot(end > p0);
+        if (behind == 0) continue;
+        const int first = __builtin_ctzll(behind);
+        c_first = c0 + first;
+        hi_first = __builtin_amdgcn_readlane(end, first);
+        lo_first = __builtin_amdgcn_readfirstlane(offsets[c_first]);
+        if (lo_first >= p0 + Cfg::BM) c_first = C;
+        break;
+    }
     int cur = 0;  // the k tile's stage, its offset
     // J: the k tile's byte of the scales, and the parity of its register set.  Without a branch inside, or the
     // compiler moves products behind later reads.
@@ -286,49 +299,77 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
     }
     __syncthreads();  // the stages are free
 
-    // ---- expand: the buckets that own rows of the tile, 16 columns of t at a time ----
-    // A fragment of 32 k is [hi | lo] of 16 columns of t against the same 16 rows of B twice.
+    // ---- expand: the buckets that own rows of the tile, 32 columns of t at a time ----
+    // A fragment of 32 k is [hi | lo] of 16 columns of t against the same 16 rows of B twice.  The next step's rows of
+    // B are on their way while one is multiplied; they go through LDS, which turns them, in two places.
     const int kq = lane >> 4, l16 = lane & 15;
     if (C > 0) {
-        int32_t *const off = (int32_t *)(smem + 16 * Cfg::B_STRIDE);
-        for (int i = tid; i <= C; i += Cfg::NT) off[i] = offsets[i];
-        __syncthreads();
-        int lo_c = 0, hi_c = C;  // first bucket that ends behind the tile's first row
-        while (lo_c < hi_c) {
-            const int mid = (lo_c + hi_c) >> 1;
-            if (off[mid + 1] > p0) hi_c = mid; else lo_c = mid + 1;
-        }
+        constexpr int PER = (32 * (Cfg::BN / 8) + Cfg::NT - 1) / Cfg::NT;  // 16-byte chunks of B per thread and step
         const int64_t n0 = ct0 * 16;
-        for (int c = lo_c; c < C && off[c] < p0 + Cfg::BM; ++c) {
-            const int lo = off[c], hi = off[c + 1];
-            if (lo == hi) continue;
-            for (int k0 = 0; k0 < R; k0 += 16) {
-                __syncthreads();
-                for (int i = tid; i < 16 * (Cfg::BN / 8); i += Cfg::NT) {
-                    const int row = i / (Cfg::BN / 8), at = i % (Cfg::BN / 8);
-                    const int64_t col = min(n0 + at * 8, (int64_t)d_out - 8);
-                    *(u32x4 *)(smem + row * Cfg::B_STRIDE + at * 16) =
-                        *(const u32x4 *)(B + ((int64_t)c * R + min(k0 + row, R - 1)) * d_out + col);
+        u32x4 b_next[PER];
+        i16x8 t[2][TM];
+        auto fetch_b = [&](int c, int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int i = tid + u * Cfg::NT, row = i / (Cfg::BN / 8), at = i % (Cfg::BN / 8);
+                b_next[u] = *(const u32x4 *)(B + ((int64_t)c * R + min(k0 + row, R - 1)) * d_out + min(n0 + at * 8, (int64_t)d_out - 8));
+            }
+        };
+        auto fetch_t = [&](int k0, int lo, int hi) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int first_row = p0 + (wm * TM + i) * 16, p = first_row + l16;
+                if (hi <= first_row || lo >= first_row + 16) continue;
+                const uint16_t *row = t2 + (int64_t)min(p, N - 1) * 2 * R + (kq >> 1) * R;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int kc = k0 + u * 16 + (kq & 1) * 8;
+                    t[u][i] = *(const i16x8 *)(row + min(kc, R - 8));
+                    if (p < lo || p >= hi || kc >= R) t[u][i] = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
                 }
-                __syncthreads();
+            }
+        };
+        int c = c_first, lo = lo_first, hi = hi_first, place = 0;
+        if (c < C) fetch_b(c, 0);
+        for (int k0 = 0; c < C;) {
+            unsigned char *const slab = smem + place * (32 * Cfg::B_STRIDE);
+            place ^= 1;
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int i = tid + u * Cfg::NT, row = i / (Cfg::BN / 8), at = i % (Cfg::BN / 8);
+                if (i < 32 * (Cfg::BN / 8)) *(u32x4 *)(slab + row * Cfg::B_STRIDE + at * 16) = b_next[u];
+            }
+            fetch_t(k0, lo, hi);
+            const int lo_now = lo, hi_now = hi, parts = R - k0 > 16 ? 2 : 1;
+            k0 += 32;
+            if (k0 >= R) {  // the next bucket with rows, as long as it begins in the tile
+                k0 = 0;
+                do {
+                    ++c;
+                    lo = hi;
+                    if (c < C) hi = __builtin_amdgcn_readfirstlane(offsets[c + 1]);
+                } while (c < C && lo < p0 + Cfg::BM && lo == hi);
+                if (lo >= p0 + Cfg::BM) c = C;
+            }
+            if (c < C) fetch_b(c, k0);
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u >= parts) break;
                 bf16x8 b[TN];
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
-                    const unsigned char *p = smem + ((kq & 1) * 8 + (l16 >> 2)) * Cfg::B_STRIDE + (wn * TN + j) * 32 + (l16 & 3) * 8;
-                    const i16x4 u = lds_read_tr16((const MOLORA_LDS void *)p), v = lds_read_tr16((const MOLORA_LDS void *)(p + 4 * Cfg::B_STRIDE));
-                    b[j] = __builtin_bit_cast(bf16x8, i16x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
+                    const unsigned char *p = slab + (u * 16 + (kq & 1) * 8 + (l16 >> 2)) * Cfg::B_STRIDE + (wn * TN + j) * 32 + (l16 & 3) * 8;
+                    const i16x4 v0 = lds_read_tr16((const MOLORA_LDS void *)p), v1 = lds_read_tr16((const MOLORA_LDS void *)(p + 4 * Cfg::B_STRIDE));
+                    b[j] = __builtin_bit_cast(bf16x8, i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
                 }
-                const int kc = k0 + (kq & 1) * 8;
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    const int first_row = p0 + (wm * TM + i) * 16, p = first_row + l16;
-                    if (hi <= first_row || lo >= first_row + 16) continue;
-                    const bool mine = p >= lo && p < hi && kc < R;
-                    i16x8 t = *(const i16x8 *)(t2 + (int64_t)min(p, N - 1) * 2 * R + (kq >> 1) * R + min(kc, R - 8));
-                    if (!mine) t = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    const int first_row = p0 + (wm * TM + i) * 16;
+                    if (hi_now <= first_row || lo_now >= first_row + 16) continue;
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], __builtin_bit_cast(bf16x8, t), acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], __builtin_bit_cast(bf16x8, t[u][i]), acc[i][j], 0, 0, 0);
                 }
             }
         }
