@@ -37,16 +37,21 @@ struct MxWorkspace {
     int32_t *offsets, *perm;
     uint16_t *t2;
     uint8_t *codes, *scales;
+    float *planes;  // at most 64 tokens: x A_r in slices of K
     size_t bytes;
 };
 inline MxWorkspace carve_mx(void *base, int64_t N, int32_t d_in, int32_t C, int32_t rank) {
     Cutter c{static_cast<unsigned char *>(base)};
-    MxWorkspace w;
-    w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
-    w.perm = c.take<int32_t>(size_t(N) * 4);
-    w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+    MxWorkspace w{};
     w.codes = c.take<uint8_t>(mx_codes(N, d_in));
     w.scales = c.take<uint8_t>(mx_scales(N, d_in));
+    if (N <= 64) {
+        w.planes = c.take<float>(size_t(molora::kMxMaxSlices) * 64 * rank * 4);
+    } else {
+        w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
+        w.perm = c.take<int32_t>(size_t(N) * 4);
+        w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+    }
     w.bytes = c.at;
     return w;
 }
@@ -113,6 +118,20 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
     return w;
 }
 
+// The dispatch step and t = x A_c of a batch of more than 64 tokens: one launch where that pays, as in molora_apply.
+inline hipError_t dispatch_shrink(const int32_t *r, const uint16_t *x, const uint16_t *A, int32_t *offsets, int32_t *perm,
+                                  uint16_t *t2, int64_t N, int32_t d_in, int32_t C, int32_t rank, hipStream_t s) {
+    const molora::Mix plain{1, C, nullptr, nullptr};
+    molora::SortArgs sort;
+    if (molora::sort_large_in_shrink(N, d_in, C, rank)) {
+        sort = molora::SortArgs{r, offsets, perm, nullptr};
+    } else {
+        const hipError_t e = molora::launch_bucket(r, offsets, perm, N, C, nullptr, s);
+        if (e != hipSuccess) return e;
+    }
+    return molora::launch_shrink(x, A, offsets, perm, t2, N, d_in, C, rank, plain, s, nullptr, sort);
+}
+
 #define MOLORA_TRY(call) \
     if ((call) != hipSuccess) return MOLORA_EHIP
 
@@ -170,7 +189,8 @@ molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, c
 
 size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank) {
     if (!apply_sizes_ok(N, d_in, d_out, C, rank) || !mx_product_ok(N, d_in, d_out)) return 0;
-    return carve_mx(nullptr, N, d_in, C, rank).bytes;
+    const size_t a = carve_mx(nullptr, N, d_in, C, rank).bytes, b = carve_mx(nullptr, N < 64 ? N : 64, d_in, C, rank).bytes;
+    return a > b ? a : b;
 }
 
 molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, const void *A, const void *B, const int32_t *r,
@@ -187,21 +207,15 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
     if (molora::ensure_device_ready() != hipSuccess) return MOLORA_EHIP;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint16_t *xb = static_cast<const uint16_t *>(x), *Ab = static_cast<const uint16_t *>(A);
-    const molora::Mix plain{1, C, nullptr, nullptr};
-    MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
-    MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
-    const bool stream_w = N <= 64;  // one read of the codes in token order, then the expand on top
-    MOLORA_TRY(molora::launch_mx_quantize(x, false, stream_w ? nullptr : w.perm, w.codes, w.scales, N, d_in, s));
-    if (stream_w) {
-        MOLORA_TRY(molora::launch_mx_gemm(w.codes, w.scales, static_cast<const uint8_t *>(wc),
-                                          static_cast<const uint8_t *>(ws), nullptr, nullptr, nullptr, nullptr, h, N, d_in,
-                                          d_out, 0, 0, s));
-        return from_hip(molora::launch_small_expand(static_cast<const uint16_t *>(B), w.t2, w.offsets, w.perm, h, N, d_in,
-                                                    d_out, C, rank, plain, s));
+    const uint8_t *wcb = static_cast<const uint8_t *>(wc), *wsb = static_cast<const uint8_t *>(ws);
+    const uint16_t *Bb = static_cast<const uint16_t *>(B);
+    if (N <= 64) {
+        MOLORA_TRY(molora::launch_mx_decode_first(xb, Ab, r, w.codes, w.scales, w.planes, N, d_in, C, rank, s));
+        return from_hip(molora::launch_mx_decode(w.codes, w.scales, wcb, wsb, Bb, r, w.planes, h, N, d_in, d_out, C, rank, s));
     }
-    return from_hip(molora::launch_mx_gemm(w.codes, w.scales, static_cast<const uint8_t *>(wc),
-                                           static_cast<const uint8_t *>(ws), static_cast<const uint16_t *>(B), w.t2,
-                                           w.offsets, w.perm, h, N, d_in, d_out, C, rank, s));
+    MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
+    MOLORA_TRY(molora::launch_mx_quantize(x, false, w.perm, w.codes, w.scales, N, d_in, s));
+    return from_hip(molora::launch_mx_gemm(w.codes, w.scales, wcb, wsb, Bb, w.t2, w.offsets, w.perm, h, N, d_in, d_out, C, rank, s));
 }
 
 size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
@@ -232,11 +246,7 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
         const molora_status st = molora_apply(x, W, A, B, r, h, N, d_in, 2 * F, C, rank, w.apply, w.apply_bytes, stream);
         return st != MOLORA_OK ? st : from_hip(molora::launch_gate(h, zb, N, F, act, s));
     }
-    if (C > 0) {
-        MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
-        MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank,
-                                         molora::Mix{1, C, nullptr, nullptr}, s));
-    }
+    if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
     return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, N, d_in, F, C, rank, act, s));
 }
 

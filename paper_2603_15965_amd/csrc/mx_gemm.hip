@@ -8,73 +8,11 @@
 #include <type_traits>
 
 #include "lds_dma.h"
-#include "mx.h"
+#include "mx_mfma.h"
 
 namespace molora {
 
 namespace {
-
-// Codes as the instruction's operand: 16 bytes a lane, the format's upper half is not read.
-__device__ __forceinline__ i32x8 mx_operand(u32x4 c) {
-    return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
-}
-// acc += W tile (first operand: a lane then holds four columns of one row of h) x x tile, scales from byte J
-template <int J>
-__device__ __forceinline__ f32x4 mx_mfma(u32x4 w, u32x4 x, f32x4 acc, uint32_t sw, uint32_t sx) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(w), mx_operand(x), acc, 4, 4, J, (int)sw, J, (int)sx);
-}
-
-// ---- a batch of at most 64 rows: one read of W ----
-// A workgroup owns 16 columns, its eight wavefronts take groups of 512 k in turn, straight from memory into
-// registers (a code tile is 1 KB, contiguous), and add their sums in LDS in a fixed order.
-template <int NR>
-__global__ __launch_bounds__(512) void mx_stream_kernel(const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs,
-                                                        const uint8_t *__restrict__ wc, const uint8_t *__restrict__ ws,
-                                                        float *__restrict__ h, int N, int d_out, int kt_n, int kg_n) {
-    __shared__ f32x4 part[8][NR][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t ct = blockIdx.x;
-    f32x4 acc[NR];
-#pragma unroll
-    for (int i = 0; i < NR; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kg = wave; kg < kg_n; kg += 8) {
-        u32x4 w[4], x[NR][4];
-        uint32_t sw, sx[NR];
-        sw = *(const uint32_t *)(ws + ((ct * kg_n + kg) * 64 + lane) * 4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {  // past the last tile: its codes again, under scales of zero codes (masked below)
-            const int kt = min(kg * 4 + j, kt_n - 1);
-            w[j] = *(const u32x4 *)(wc + ((ct * kt_n + kt) * 64 + lane) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            sx[i] = *(const uint32_t *)(xs + (((int64_t)i * kg_n + kg) * 64 + lane) * 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int kt = min(kg * 4 + j, kt_n - 1);
-                x[i][j] = *(const u32x4 *)(xc + (((int64_t)i * kt_n + kt) * 64 + lane) * 16);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            acc[i] = mx_mfma<0>(w[0], x[i][0], acc[i], sw, sx[i]);
-            if (kg * 4 + 1 < kt_n) acc[i] = mx_mfma<1>(w[1], x[i][1], acc[i], sw, sx[i]);
-            if (kg * 4 + 2 < kt_n) acc[i] = mx_mfma<2>(w[2], x[i][2], acc[i], sw, sx[i]);
-            if (kg * 4 + 3 < kt_n) acc[i] = mx_mfma<3>(w[3], x[i][3], acc[i], sw, sx[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NR; ++i) part[wave][i][lane] = acc[i];
-    __syncthreads();
-    if (wave < NR) {
-        f32x4 sum = part[0][wave][lane];
-#pragma unroll
-        for (int w = 1; w < 8; ++w) sum += part[w][wave][lane];
-        const int row = wave * 16 + (lane & 15);
-        const int64_t col = ct * 16 + (lane >> 4) * 4;
-        if (row < N && col < d_out) *(f32x4 *)(h + (int64_t)row * d_out + col) = sum;
-    }
-}
 
 // ---- larger batches: output tiles ----
 // BM x BN output tile, WM x WN wavefronts of TM x TN tiles of 16 x 16.  A stage is 128 k of both sides, brought to
@@ -420,29 +358,31 @@ hipError_t launch_mx_tiles(const uint8_t *xc, const uint8_t *xs, const uint8_t *
 using Mx256 = MxCfg<2, 4, 8, 4, 4>;   // 256 x 256, one workgroup per compute unit
 using MxWide = MxCfg<2, 2, 8, 4, 3>;  // 256 x 128, two
 using Mx128 = MxCfg<2, 2, 4, 4, 3>;   // 128 x 128, three
+using Mx128Deep = MxCfg<2, 2, 4, 4, 4>;  // the same with a stage more, two
 using MxLow = MxCfg<1, 4, 4, 2, 4>;   // 64 x 128, four
 using Mx64 = MxCfg<2, 2, 2, 2, 4>;    // 64 x 64, five
 
 namespace {
 // The tile from the sizes: the least of the costs below (us).  Tiles run in rounds of 256 compute units x workgroups per
 // unit; a whole round costs a start and an end and a time per k tile of 128, the last one parts of both that
-// grow with its share of the places.  Coefficients: non-negative least squares of the relative error over 96
-// shapes, 65 .. 16384 rows, 256 .. 12288 deep, 1024 .. 12288 wide, every configuration timed on each.  The choice is
-// 2 % behind the best configuration there (geometric mean), the large tiles alone 60 %, the smallest alone 35 %.
+// grow with its share of the places.  Coefficients: non-negative least squares of the relative error over 128
+// shapes, 65 .. 16384 rows, 256 .. 12288 deep, 1024 .. 12288 wide, every configuration timed on each with its operands
+// from HBM.  The choice is 3 % behind the best configuration there (geometric mean, but for a few timings that were
+// disturbed at most 26 %).
 struct MxCost {
     int bm, bn, per_cu;
     double once, round, part, last, k_round, k_part, k_last;
 };
 constexpr MxCost kMxCosts[] = {
-    {256, 256, 1, 3.8, 11.4, 4.3, 1.4, 0.784, 0.512, 0.314}, {256, 128, 2, 7.7, 9.4, 0.0, 2.3, 0.755, 0.316, 0.331},
-    {128, 128, 3, 3.3, 6.8, 1.7, 4.3, 0.598, 0.217, 0.263},  {64, 128, 4, 3.8, 4.3, 0.1, 2.8, 0.561, 0.119, 0.309},
-    {64, 64, 5, 3.2, 2.7, 0.0, 2.0, 0.444, 0.091, 0.291}};
+    {256, 256, 1, 2.2, 12.0, 5.4, 4.3, 0.762, 0.523, 0.163}, {256, 128, 2, 7.3, 9.5, 0.0, 4.4, 0.774, 0.322, 0.341},
+    {128, 128, 3, 3.5, 6.3, 1.2, 4.3, 0.651, 0.232, 0.364},  {128, 128, 2, 4.4, 4.4, 0.7, 2.5, 0.457, 0.185, 0.197},
+    {64, 128, 4, 3.7, 3.9, 0.0, 3.0, 0.588, 0.125, 0.389},   {64, 64, 5, 3.0, 2.4, 0.0, 2.2, 0.447, 0.100, 0.337}};
 
 int mx_tile_choice(int64_t N, int d_in, int d_out) {
     const double kt = mx_k_tiles(d_in);
     double best = 1e30;
     int pick = 0;
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < 6; ++i) {
         const MxCost &c = kMxCosts[i];
         const int64_t tiles = ((N + c.bm - 1) / c.bm) * (((int64_t)d_out + c.bn - 1) / c.bn), slots = 256 * c.per_cu;
         const double full = (double)(tiles / slots), last = (double)(tiles % slots) / (double)slots, part = last > 0 ? 1 : 0;
@@ -460,23 +400,14 @@ hipError_t launch_mx_gemm(const uint8_t *xc, const uint8_t *xs, const uint8_t *w
                           const uint16_t *t2, const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in,
                           int d_out, int C, int rank, hipStream_t s) {
     if (N == 0) return hipSuccess;
-    if (N <= 64 && C == 0 && perm == nullptr) {
-        const dim3 grid((unsigned)((d_out + 15) / 16)), block(512);
-        const int kt = mx_k_tiles(d_in), kg = mx_k_groups(d_in);
-#define MOLORA_MX_STREAM(NR) hipLaunchKernelGGL((mx_stream_kernel<NR>), grid, block, 0, s, xc, xs, wc, ws, h, (int)N, d_out, kt, kg)
-        if (N <= 16) MOLORA_MX_STREAM(1);
-        else if (N <= 32) MOLORA_MX_STREAM(2);
-        else if (N <= 48) MOLORA_MX_STREAM(3);
-        else MOLORA_MX_STREAM(4);
-#undef MOLORA_MX_STREAM
-        return hipGetLastError();
-    }
+    if (N <= 64 && C == 0) return launch_mx_decode(xc, xs, wc, ws, nullptr, nullptr, nullptr, h, N, d_in, d_out, 0, 0, s);
 #define MOLORA_MX_TILES(CFG) launch_mx_tiles<CFG>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, s)
     switch (mx_tile_choice(N, d_in, d_out)) {  // the order of kMxCosts
         case 0: return MOLORA_MX_TILES(Mx256);
         case 1: return MOLORA_MX_TILES(MxWide);
         case 2: return MOLORA_MX_TILES(Mx128);
-        case 3: return MOLORA_MX_TILES(MxLow);
+        case 3: return MOLORA_MX_TILES(Mx128Deep);
+        case 4: return MOLORA_MX_TILES(MxLow);
         default: return MOLORA_MX_TILES(Mx64);
     }
 #undef MOLORA_MX_TILES
