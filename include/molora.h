@@ -482,7 +482,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * never stored unless pre (DEVICE fp32 [N][2 F], may be NULL) asks for it: the backward pass needs it.
  * Without adapters: A, B, r NULL, C = rank = 0.  act: MOLORA_ACT_*.  F >= 8 and a multiple of 8; x, W
  * and h in bf16 below 4 GiB each.  workspace DEVICE, 256-byte aligned, of
- * molora_apply_gated_workspace_bytes(...) bytes (0 and NULL without adapters), never less for
+ * molora_apply_gated_workspace_bytes(...) bytes (where that is 0 it may be NULL), never less for
  * more tokens.  Errors as molora_apply.
  *
  * molora_gated_backward: the gradients of a scalar loss whose gradient with respect to z is dz (DEVICE bf16

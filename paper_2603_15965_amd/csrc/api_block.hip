@@ -1,6 +1,7 @@
 // C ABI of the feed-forward block: 4-bit microscaled products and the gated block.  Argument checking and the
 // order of launches, no arithmetic.
 #include "api_util.h"
+#include "decode_body.h"
 #include "mx.h"
 
 namespace {
@@ -20,6 +21,8 @@ inline bool mx_product_ok(int64_t N, int32_t d_in, int32_t d_out) {
     return d_out >= 8 && d_out % 8 == 0 && mx_sizes_ok(N, d_in) && mx_sizes_ok(d_out, d_in) &&
            ((N + 127) / 128) * ((int64_t(d_out) + 127) / 128) < molora::kMxMaxBlocks;
 }
+
+constexpr int64_t kDecode = 64;  // batches that are one read of the base weight
 
 struct Cutter {  // pieces of a workspace, each 256-byte aligned
     unsigned char *base;
@@ -45,8 +48,8 @@ inline MxWorkspace carve_mx(void *base, int64_t N, int32_t d_in, int32_t C, int3
     MxWorkspace w{};
     w.codes = c.take<uint8_t>(mx_codes(N, d_in));
     w.scales = c.take<uint8_t>(mx_scales(N, d_in));
-    if (N <= 64) {
-        w.planes = c.take<float>(size_t(molora::kMxMaxSlices) * 64 * rank * 4);
+    if (N <= kDecode) {
+        w.planes = c.take<float>(size_t(molora::kMaxSlices) * 64 * rank * 4);
     } else {
         w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
         w.perm = c.take<int32_t>(size_t(N) * 4);
@@ -68,30 +71,38 @@ inline bool adapters_given(const void *A, const void *B, const int32_t *r, int32
     return C == 0 ? !A && !B && !r : A && B && r;
 }
 
-constexpr int64_t kGatedStream = 64;  // batches whose projection streams W: molora_apply, then the activation
-
 struct GatedWorkspace {
-    void *apply;  // molora_apply's own
-    size_t apply_bytes;
-    float *pre;
     int32_t *offsets, *perm;
     uint16_t *t2;
+    float *base, *planes;  // at most 64 tokens: x W, in slices of K
+    int slices;
     size_t bytes;
 };
 inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
     Cutter c{static_cast<unsigned char *>(base)};
     GatedWorkspace w{};
-    if (C > 0 && N <= kGatedStream) {
-        w.apply_bytes = molora_apply_workspace_bytes(N, d_in, 2 * F, C, rank);
-        w.apply = c.take<void>(w.apply_bytes);
-        w.pre = c.take<float>(size_t(N) * 2 * F * 4);
-    } else if (C > 0) {
+    if (C > 0) {
         w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
         w.perm = c.take<int32_t>(size_t(N) * 4);
         w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
     }
+    if (N <= kDecode) {
+        const size_t plane = size_t(N) * 2 * F * 4;
+        w.slices = molora::small_base_slices(N, d_in, 2 * F, C);
+        w.base = c.take<float>(plane);
+        if (w.slices > 1) w.planes = c.take<float>(plane * (w.slices - 1));
+    }
     w.bytes = c.at;
     return w;
+}
+// Room for any batch of up to N tokens: one of a few tokens may be cut into more slices than one of 64.
+inline size_t gated_workspace_up_to(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
+    size_t most = carve_gated(nullptr, N, d_in, F, C, rank).bytes;
+    for (int64_t n = 1; n <= N && n <= kDecode; ++n) {
+        const size_t b = carve_gated(nullptr, n, d_in, F, C, rank).bytes;
+        most = b > most ? b : most;
+    }
+    return most;
 }
 
 struct BackwardWorkspace {
@@ -189,7 +200,7 @@ molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, c
 
 size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank) {
     if (!apply_sizes_ok(N, d_in, d_out, C, rank) || !mx_product_ok(N, d_in, d_out)) return 0;
-    const size_t a = carve_mx(nullptr, N, d_in, C, rank).bytes, b = carve_mx(nullptr, N < 64 ? N : 64, d_in, C, rank).bytes;
+    const size_t a = carve_mx(nullptr, N, d_in, C, rank).bytes, b = carve_mx(nullptr, N < kDecode ? N : kDecode, d_in, C, rank).bytes;
     return a > b ? a : b;
 }
 
@@ -209,7 +220,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
     const uint16_t *xb = static_cast<const uint16_t *>(x), *Ab = static_cast<const uint16_t *>(A);
     const uint8_t *wcb = static_cast<const uint8_t *>(wc), *wsb = static_cast<const uint8_t *>(ws);
     const uint16_t *Bb = static_cast<const uint16_t *>(B);
-    if (N <= 64) {
+    if (N <= kDecode) {
         MOLORA_TRY(molora::launch_mx_decode_first(xb, Ab, r, w.codes, w.scales, w.planes, N, d_in, C, rank, s));
         return from_hip(molora::launch_mx_decode(w.codes, w.scales, wcb, wsb, Bb, r, w.planes, h, N, d_in, d_out, C, rank, s));
     }
@@ -220,9 +231,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
 
 size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
     if (!gated_sizes_ok(N, d_in, F, C, rank, 0)) return 0;
-    const size_t a = carve_gated(nullptr, N, d_in, F, C, rank).bytes;
-    const size_t b = carve_gated(nullptr, N < kGatedStream ? N : kGatedStream, d_in, F, C, rank).bytes;
-    return a > b ? a : b;
+    return gated_workspace_up_to(N, d_in, F, C, rank);
 }
 
 molora_status molora_apply_gated(const void *x, const void *W, const void *A, const void *B, const int32_t *r, void *z,
@@ -230,7 +239,8 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
                                  void *workspace, size_t workspace_bytes, void *stream) {
     if (!gated_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
     if (N == 0) return MOLORA_OK;
-    if (!x || !W || !z || !adapters_given(A, B, r, C) || (C > 0 && !workspace)) return MOLORA_EINVAL;
+    if (!x || !W || !z || !adapters_given(A, B, r, C)) return MOLORA_EINVAL;
+    if (!workspace && carve_gated(nullptr, N, d_in, F, C, rank).bytes > 0) return MOLORA_EINVAL;
     if (!aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(r) || !aligned16(z) ||
         !aligned16(pre) || !aligned256(workspace))
         return MOLORA_EALIGN;
@@ -241,10 +251,12 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
     uint16_t *zb = static_cast<uint16_t *>(z);
     const uint16_t *xb = static_cast<const uint16_t *>(x), *Wb = static_cast<const uint16_t *>(W);
     const uint16_t *Ab = static_cast<const uint16_t *>(A), *Bb = static_cast<const uint16_t *>(B);
-    if (C > 0 && N <= kGatedStream) {
-        float *h = pre != nullptr ? pre : w.pre;
-        const molora_status st = molora_apply(x, W, A, B, r, h, N, d_in, 2 * F, C, rank, w.apply, w.apply_bytes, stream);
-        return st != MOLORA_OK ? st : from_hip(molora::launch_gate(h, zb, N, F, act, s));
+    if (N <= kDecode) {
+        float *base = pre != nullptr ? pre : w.base;
+        MOLORA_TRY(molora::launch_small_shrink_base(xb, Wb, Ab, base, w.t2, N, d_in, 2 * F, C, C > 0 ? rank : 8,
+                                                    molora::Mix{1, C, nullptr, nullptr},
+                                                    molora::SortArgs{r, w.offsets, w.perm, nullptr}, s, false, w.planes, w.slices));
+        return from_hip(molora::launch_gated_finish(base, w.planes, w.slices, Bb, r, w.t2, w.perm, zb, pre, N, F, C, rank, act, s));
     }
     if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
     return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, N, d_in, F, C, rank, act, s));

@@ -195,7 +195,11 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
 int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
 
 // ---- around the gated block (gated.hip) ----
-hipError_t launch_gate(const float *pre, uint16_t *z, int64_t N, int F, int act, hipStream_t s);
+// at most 64 tokens (gated_decode.hip): h = base + the planes of the other slices + t B_r, z from it, h stored where
+// pre != nullptr (which may be base).  t2, perm: launch_small_shrink_base's; C = 0: without adapters
+hipError_t launch_gated_finish(const float *base, const float *planes, int slices, const uint16_t *B, const int32_t *r,
+                               const uint16_t *t2, const int32_t *perm, uint16_t *z, float *pre, int64_t N, int F, int C, int rank,
+                               int act, hipStream_t s);
 // dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F]; rows N .. padded - 1 are zero
 hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
                                 int act, hipStream_t s);
@@ -222,10 +226,12 @@ hipError_t launch_small_batch_gemm(const uint16_t *x, const uint16_t *W, const u
 hipError_t launch_small_shrink_base(const uint16_t *x, const uint16_t *W, const uint16_t *A, float *h,
                                     uint16_t *t_out, int64_t N, int d_in, int d_out, int C, int rank,
                                     Mix mix, SortArgs sort, hipStream_t s, bool w_packed = false,
-                                    float *planes = nullptr);
+                                    float *planes = nullptr, int slices = 0);
+// (slices > 0: as many, else small_base_ksplit's; sort.r == nullptr with C = 0: x W alone)
 // K slices of x W in that launch when it is given room for the sums of all but the first, planes
 // [slices - 1][N][d_out] (fp32), which launch_small_expand then adds; 1: K is not cut
 int small_base_ksplit(int64_t N, int d_in, int d_out, int C, int rank);
+int small_base_slices(int64_t N, int d_in, int d_out, int C);  // whatever the rank; C = 0: no adapters
 // W for launch_small_shrink_base(..., w_packed = true): slabs of 16 rows, inside a slab groups of
 // gc = small_pack_cols(d_out) columns one after the other (0: this d_out has no packed form)
 int small_pack_cols(int d_out);

@@ -1,5 +1,4 @@
-// Around the gated block z = act(g) u, [g | u] = h = x W + (x A_r) B_r: the activation by itself (batches whose
-// projection streams W), and what its backward pass needs beside the GEMMs:
+// The backward pass of the gated block z = act(g) u, [g | u] = h = x W + (x A_r) B_r, beside its GEMMs:
 //
 //     dh = [dz u act'(g) | dz act(g)],   dA_c = x_c^T (dh_c B_c^T),   dB_c = (x_c A_c)^T dh_c
 #include "gate.h"
@@ -10,17 +9,6 @@ namespace molora {
 namespace {
 
 // One thread takes four columns of a row.
-__global__ __launch_bounds__(256) void gate_kernel(const float *__restrict__ pre, uint16_t *__restrict__ z, int64_t items,
-                                                   int F, int act) {
-    const int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (it >= items) return;
-    const int per = F / 4;
-    const int64_t row = it / per;
-    const int col = (int)(it % per) * 4;
-    const float *h = pre + row * 2 * F + col;
-    *(u32x2 *)(z + row * F + col) = bf16x4_bits(gate4(*(const f32x4 *)h, *(const f32x4 *)(h + F), act));
-}
-
 // dh is rounded to bf16 here: it is an operand of the matrix instructions in every gradient that follows.  (h comes
 // in fp32: with g and u rounded too, the gradients would be 1.9 instead of 1.4 times as far from their exact
 // values as their own rounding to bf16 puts them.)
@@ -177,13 +165,6 @@ hipError_t launch_zero(void *dst, int64_t bytes, hipStream_t s) {
     const int64_t n = bytes / 16, blocks = (n + 255) / 256;
     if (n > 0)
         hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, (u32x4 *)dst, n);
-    return hipGetLastError();
-}
-
-hipError_t launch_gate(const float *pre, uint16_t *z, int64_t N, int F, int act, hipStream_t s) {
-    const int64_t items = N * (F / 4), blocks = (items + 255) / 256;
-    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
-    if (blocks > 0) hipLaunchKernelGGL(gate_kernel, dim3((unsigned)blocks), dim3(256), 0, s, pre, z, items, F, act);
     return hipGetLastError();
 }
 

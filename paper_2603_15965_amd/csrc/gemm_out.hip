@@ -14,8 +14,8 @@ hipError_t launch_out(const uint16_t *x, const uint16_t *W, const uint16_t *B, c
     const int cols = OUT == kOutGated ? d_out / 2 : d_out, per = OUT == kOutGated ? Cfg::BN / 2 : Cfg::BN;
     const int tiles_n = (cols + per - 1) / per;
     const unsigned blocks = (unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8);
-    launch_base_kernel(fused_gemm_kernel<Cfg, OUT>, dim3(blocks), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm,
-                       h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
+    constexpr auto kernel = fused_gemm_kernel<Cfg, OUT>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
     return hipGetLastError();
 }
 

@@ -38,10 +38,8 @@ hipError_t launch_mx_gemm(const uint8_t *xc, const uint8_t *xs, const uint8_t *w
                           int d_out, int C, int rank, hipStream_t s);
 
 // A batch of at most 64 tokens in two launches (mx_decode.hip).  The first: the rows' codes and scales, in token order,
-// and x_i A_{r(i)} in mx_decode_slices(...) slices of K, planes [slices][64][rank] fp32 (rows of tokens without
-// adapter are not written).  The second: h = Q(x) Q(W) + (x A_r) B_r; with C = 0 the product alone.
-constexpr int kMxMaxSlices = 4;
-int mx_decode_slices(int64_t N, int d_in, int C, int rank);
+// and x_i A_{r(i)} in slices of K (decode_body.h), planes [slices][64][rank] fp32 (rows of tokens without adapter
+// are not written).  The second: h = Q(x) Q(W) + (x A_r) B_r; with C = 0 the product alone.
 hipError_t launch_mx_decode_first(const uint16_t *x, const uint16_t *A, const int32_t *r, uint8_t *codes, uint8_t *scales,
                                   float *planes, int64_t N, int d_in, int C, int rank, hipStream_t s);
 hipError_t launch_mx_decode(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, const uint8_t *ws, const uint16_t *B,

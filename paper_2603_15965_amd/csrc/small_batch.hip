@@ -965,7 +965,7 @@ hipError_t launch_shrink_base(const uint16_t *x, const uint16_t *W, const uint16
     if (PACKED && d_out % SbGeom<TN>::COLS != 0) return hipErrorInvalidValue;  // whole groups only
     const int shrink_groups = (mix.k * rank + 31) / 32;
     const int gemm_groups = (d_out + SbGeom<TN>::COLS - 1) / SbGeom<TN>::COLS;
-    const int places = sorted_places(N, C, shrink_groups, gemm_groups * ksplit);
+    const int places = C > 0 ? sorted_places(N, C, shrink_groups, gemm_groups * ksplit) : 0;
     const int n_shrink = shrink_groups * places;
     auto kern = shrink_base_small_kernel<TM, TN, PACKED>;
     constexpr size_t lds_bytes = ShrinkBaseKernel<TM, TN, PACKED>::LDS;
@@ -987,8 +987,11 @@ hipError_t launch_shrink_base(const uint16_t *x, const uint16_t *W, const uint16
 // Ranks above 32 have the two launches as entry points of their own, without scratch and bit for bit
 // equal to molora_apply, and stay unsplit.
 int small_base_ksplit(int64_t N, int d_in, int d_out, int C, int rank) {
+    return rank > 32 ? 1 : small_base_slices(N, d_in, d_out, C);
+}
+int small_base_slices(int64_t N, int d_in, int d_out, int C) {
     const int64_t groups = (d_out + 63) / 64, n_shrink = N < C ? N : C;
-    if (N < 1 || N > 64 || rank > 32 || groups + n_shrink >= 256) return 1;
+    if (N < 1 || N > 64 || groups + n_shrink >= 256) return 1;
     const int64_t pieces = (d_in + 63) / 64;
     auto units = [&](int64_t ks) { return ((pieces + ks - 1) / ks + kSbWaves - 1) / kSbWaves; };
     int64_t ks = (256 - n_shrink) / groups;
@@ -1000,11 +1003,11 @@ int small_base_ksplit(int64_t N, int d_in, int d_out, int C, int rank) {
 // N <= 64: dispatch + shrink + h = x W in one launch (sort.r, sort.offsets, sort.perm required)
 hipError_t launch_small_shrink_base(const uint16_t *x, const uint16_t *W, const uint16_t *A, float *h,
                                     uint16_t *t_out, int64_t N, int d_in, int d_out, int C, int rank,
-                                    Mix mix, SortArgs sort, hipStream_t s, bool w_packed, float *planes) {
-    if (N < 1 || N > 64 || mix.k != 1 || !sort.r || !sort.offsets || !sort.perm) return hipErrorInvalidValue;
+                                    Mix mix, SortArgs sort, hipStream_t s, bool w_packed, float *planes, int slices) {
+    if (N < 1 || N > 64 || mix.k != 1 || (C > 0 && (!sort.r || !sort.offsets || !sort.perm))) return hipErrorInvalidValue;
     if (w_packed && small_pack_cols(d_out) == 0) return hipErrorInvalidValue;
     // K slices: columns in groups of 64 (half the x traffic of groups of 32 per byte of W)
-    const int ks = planes != nullptr && !w_packed ? small_base_ksplit(N, d_in, d_out, C, rank) : 1;
+    const int ks = planes == nullptr || w_packed ? 1 : slices > 0 ? slices : small_base_ksplit(N, d_in, d_out, C, rank);
     const bool narrow = ks == 1 && sb_narrow_one_tile(d_out);
 #define MOLORA_SBB(TM, TN)                                                                                          \
     (w_packed ? launch_shrink_base<TM, TN, true>(x, W, A, h, t_out, (int)N, d_in, d_out, C, rank, mix, sort, s, 1, nullptr) \

@@ -76,7 +76,7 @@ def test_operand_and_workspace_sizes(lib):
         got = [f(n, 512, *last) for n in (0, 1, 7, 8, 9, 63, 64, 65, 100, 511, 512, 513, 4096, 20000)]
         assert got == sorted(got) and got[1] > 0, f
         assert f(16, 512, last[0], 8, 12) == 0 and f(16, 510, *last) == 0 and f(16, 512, last[0], 1025, 8) == 0 and f(-1, 512, *last) == 0
-    assert lib.molora_apply_gated_workspace_bytes(300, 512, 320, 0, 0) == 0
+    assert lib.molora_apply_gated_workspace_bytes(300, 512, 320, 0, 0) >= 64 * 640 * 4   # x W of a batch of 64
     assert lib.molora_gated_backward_workspace_bytes(300, 512, 320, 0, 0) > 0
     assert lib.molora_apply_gated_workspace_bytes(300, 512, 320, 0, 8) == 0
     assert lib.molora_apply_gated_workspace_bytes(1 << 20, 2048, 320, 4, 8) == 0   # x of 4 GiB
