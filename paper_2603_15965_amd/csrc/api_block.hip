@@ -4,6 +4,8 @@
 #include "decode_body.h"
 #include "mx.h"
 
+#include <algorithm>
+
 namespace {
 
 // Rows and k of a microscaled operand.
@@ -108,6 +110,8 @@ inline size_t gated_workspace_up_to(int64_t N, int32_t d_in, int32_t F, int32_t 
 struct BackwardWorkspace {
     int32_t *offsets, *perm;
     uint16_t *t2, *s2, *dh, *xt, *wt, *at, *bt;
+    float *planes;
+    size_t outer_a;  // floats of planes that dA takes
     size_t bytes;
 };
 inline int64_t padded_rows(int64_t N) { return (N + 7) & ~int64_t(7); }
@@ -125,6 +129,12 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
     w.dh = c.take<uint16_t>(size_t(padded_rows(N)) * 2 * F * 2);
     w.xt = c.take<uint16_t>(size_t(padded_rows(N)) * d_in * 2);
     w.wt = c.take<uint16_t>(size_t(d_in) * 2 * F * 2);
+    // fp32 sums of one product at a time: slices of K of dx and dW, pieces of the rows of dA and dB
+    size_t floats = size_t(molora::gemm_plane_floats(N, d_in));
+    floats = std::max(floats, size_t(molora::gemm_plane_floats(d_in, 2 * int64_t(F))));
+    w.outer_a = C > 0 ? round256(molora::grouped_outer_floats(N, d_in, C, rank) * 4) / 4 : 0;
+    if (C > 0) floats = std::max(floats, w.outer_a + molora::grouped_outer_floats(N, 2 * F, C, rank));
+    w.planes = c.take<float>(floats * 4);
     w.bytes = c.at;
     return w;
 }
@@ -143,8 +153,10 @@ inline hipError_t dispatch_shrink(const int32_t *r, const uint16_t *x, const uin
     return molora::launch_shrink(x, A, offsets, perm, t2, N, d_in, C, rank, plain, s, nullptr, sort);
 }
 
-#define MOLORA_TRY(call) \
-    if ((call) != hipSuccess) return MOLORA_EHIP
+#define MOLORA_TRY(call)                              \
+    do {                                              \
+        if ((call) != hipSuccess) return MOLORA_EHIP; \
+    } while (0)
 
 }  // namespace
 
@@ -292,30 +304,35 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
     const uint16_t *Ab = static_cast<const uint16_t *>(A), *Bb = static_cast<const uint16_t *>(B);
     const molora::Mix plain{1, C, nullptr, nullptr};
     const int64_t Np = padded_rows(N);
+    // the operands whose k runs down their columns, turned
+    molora::TransposeJob turn[molora::kMaxTransposes];
+    int turns = 0;
+    if (C > 0 && (dx || dA)) turn[turns++] = {Bb, w.bt, C, rank, 2 * F, rank};
+    if (C > 0 && dx) turn[turns++] = {Ab, w.at, C, d_in, rank, d_in};
+    if (dx) turn[turns++] = {Wb, w.wt, 1, d_in, 2 * F, d_in};
+    if (dW) turn[turns++] = {xb, w.xt, 1, N, d_in, Np};
+    MOLORA_TRY(molora::launch_transposes(turn, turns, s));
     MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
     if (C > 0) {
-        MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
-        if (dx || dA) {  // s = dh B^T
-            MOLORA_TRY(molora::launch_transpose(Bb, w.bt, C, rank, 2 * F, rank, s));
+        if (dB && N > kDecode)
+            MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
+        else
+            MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
+        if (dB && N <= kDecode) MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
+        if (dx || dA)  // s = dh B^T
             MOLORA_TRY(molora::launch_shrink(w.dh, w.bt, w.offsets, w.perm, w.s2, N, 2 * F, C, rank, plain, s));
-        }
-        if (dB) MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
-        if (dA)
-            MOLORA_TRY(molora::launch_grouped_outer(xb, w.s2, w.offsets, w.perm, static_cast<uint16_t *>(dA), N, d_in, C, rank, false, s));
-        if (dB)
-            MOLORA_TRY(molora::launch_grouped_outer(w.dh, w.t2, w.offsets, w.perm, static_cast<uint16_t *>(dB), N, 2 * F, C, rank, true, s));
+        molora::GroupedOuter outer[2];
+        int outers = 0;
+        if (dA) outer[outers++] = {xb, w.s2, static_cast<uint16_t *>(dA), w.planes, d_in, false};
+        if (dB) outer[outers++] = {w.dh, w.t2, static_cast<uint16_t *>(dB), w.planes + w.outer_a, 2 * F, true};
+        MOLORA_TRY(molora::launch_grouped_outers(outer, outers, w.offsets, w.perm, N, C, rank, s));
     }
-    if (dx) {
-        MOLORA_TRY(molora::launch_transpose(Wb, w.wt, 1, d_in, 2 * F, d_in, s));
-        if (C > 0) MOLORA_TRY(molora::launch_transpose(Ab, w.at, C, d_in, rank, d_in, s));
+    if (dx)
         MOLORA_TRY(molora::launch_gemm_bf16(w.dh, w.wt, w.at, w.s2, w.offsets, C > 0 ? w.perm : nullptr,
-                                            static_cast<uint16_t *>(dx), N, 2 * F, d_in, C, rank, s));
-    }
-    if (dW) {
-        MOLORA_TRY(molora::launch_transpose(xb, w.xt, 1, N, d_in, Np, s));
-        MOLORA_TRY(molora::launch_gemm_bf16(w.xt, w.dh, nullptr, nullptr, nullptr, nullptr, static_cast<uint16_t *>(dW), d_in,
-                                            (int)Np, 2 * F, 0, 0, s));
-    }
+                                            static_cast<uint16_t *>(dx), w.planes, N, 2 * F, d_in, C, rank, s));
+    if (dW)
+        MOLORA_TRY(molora::launch_gemm_bf16(w.xt, w.dh, nullptr, nullptr, nullptr, nullptr, static_cast<uint16_t *>(dW), w.planes,
+                                            d_in, (int)Np, 2 * F, 0, 0, s));
     return MOLORA_OK;
 }
 

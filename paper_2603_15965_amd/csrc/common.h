@@ -183,10 +183,21 @@ void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile
 
 // ---- the fused GEMM with other outputs (gemm_out.hip); offsets, perm and t2 as launch_fused_gemm, or perm == nullptr and
 // C = 0: rows in order, without adapters.  Operands below 4 GiB each (fused_gemm_sizes_ok with a tile forced). ----
-// out = x W + t B_c in bf16
+// out = x W + t B_c in bf16.  planes: scratch of gemm_plane_floats(N, d_out) floats, for K in slices where the output has
+// too few tiles for the chip
+constexpr int kMaxGemmSlices = 8;
+constexpr int64_t kMaxPlaneFloats = int64_t(8) << 20;
+inline int64_t gemm_plane_floats(int64_t N, int64_t d_out) {
+    const int64_t f = kMaxGemmSlices * N * d_out;
+    return f < kMaxPlaneFloats ? f : kMaxPlaneFloats;
+}
 hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
-                            const int32_t *offsets, const int32_t *perm, uint16_t *out, int64_t N, int d_in, int d_out,
-                            int C, int rank, hipStream_t s);
+                            const int32_t *offsets, const int32_t *perm, uint16_t *out, float *planes, int64_t N, int d_in,
+                            int d_out, int C, int rank, hipStream_t s);
+struct GemmSlices {
+    int slices, config;
+};
+GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
 // h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                              const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, int64_t N, int d_in,
@@ -203,14 +214,29 @@ hipError_t launch_gated_finish(const float *base, const float *planes, int slice
 // dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F]; rows N .. padded - 1 are zero
 hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
                                 int act, hipStream_t s);
-// dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on
-hipError_t launch_transpose(const uint16_t *src, uint16_t *dst, int64_t batch, int64_t rows, int64_t cols, int64_t padded,
-                            hipStream_t s);
+// dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on; in one launch
+constexpr int kMaxTransposes = 4;
+struct TransposeJob {
+    const uint16_t *src;
+    uint16_t *dst;
+    int64_t batch, rows, cols, padded;
+};
+hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s);
 // out[c] = sum over the positions p of bucket c of outer(y[perm[p]], s_p), bf16: [D][R], or [R][D] when flat;
-// y [N][D], s2 [N][2 R] in the layout of the shrink's output.  Empty buckets give zeros.
-hipError_t launch_grouped_outer(const uint16_t *y, const uint16_t *s2, const int32_t *offsets, const int32_t *perm,
-                                uint16_t *out, int64_t N, int D, int C, int R, bool flat, hipStream_t s);
-
+// y [N][D], s2 [N][2 R] in the layout of the shrink's output.  Empty buckets give zeros.  planes: scratch of
+// grouped_outer_floats(...) floats.
+struct GroupedOuter {
+    const uint16_t *y, *s2;
+    uint16_t *out;
+    float *planes;
+    int D;
+    bool flat;
+};
+size_t grouped_outer_floats(int64_t N, int D, int C, int R);
+hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t *offsets, const int32_t *perm, int64_t N, int C,
+                                 int R, hipStream_t s);
+// out [n] bf16 = the sum of `count` planes of n floats (a multiple of 8)
+hipError_t launch_sum_planes(const float *planes, uint16_t *out, int64_t n, int count, hipStream_t s);
 hipError_t launch_zero(void *dst, int64_t bytes, hipStream_t s);  // bytes a multiple of 16
 
 // columns per workgroup of the streaming kernel, 32 or 64

@@ -72,11 +72,11 @@ constexpr GemmCost kGemmCosts[] = {
 };
 constexpr int kGemmConfigs = sizeof(kGemmCosts) / sizeof(kGemmCosts[0]);
 
-double tiled_cost(const GemmCost &g, int64_t N, int d_in, int d_out, int C, int R) {
-    const int64_t tiles = ((N + g.bm - 1) / g.bm) * ((d_out + g.bn - 1) / g.bn);
+double tiled_cost(const GemmCost &g, int64_t N, int d_in, int d_out, int C, int R, int slices = 1) {
+    const int64_t tiles = ((N + g.bm - 1) / g.bm) * ((d_out + g.bn - 1) / g.bn) * slices;
     const int64_t slots = (int64_t)256 * g.per_cu, full = tiles / slots;
     const double last = (double)(tiles % slots) / (double)slots, part = last > 0 ? 1 : 0;
-    const double kt = (d_in + 63) / 64;
+    const double kt = (d_in + 64 * slices - 1) / (64 * slices);
     const double segs = fmin((double)C, 1.0 + (double)g.bm * C / (double)N);  // buckets that own rows of a tile
     const double expand = segs * ((R + 15) / 16) / 4 + (R + 31) / 32;
     return g.once + g.per_round * (double)full + g.partial * part + kt * (g.k_round * (double)full + g.k_few * part + g.k_full * last) +
@@ -112,6 +112,25 @@ int gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming = t
 }  // namespace
 
 int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) { return gemm_choice(N, d_in, d_out, C, R, false); }
+
+// The same with K in slices: their sums cost a second launch and a trip through memory.
+GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) {
+    GemmSlices pick{1, gemm_choice(N, d_in, d_out, C, R, false)};
+    double best = tiled_cost(kGemmCosts[pick.config], N, d_in, d_out, C, R);
+    for (int slices = 2; slices <= kMaxGemmSlices; ++slices) {
+        const double floats = (double)slices * (double)N * d_out;
+        if (floats > (double)kMaxPlaneFloats || d_in < slices * 256) break;
+        for (int i = 0; i < kGemmConfigs; ++i) {
+            // (4 MB a microsecond written and read, and the launch)
+            const double cost = tiled_cost(kGemmCosts[i], N, d_in, d_out, C, R, slices) + 4.0 + floats * 8 / 4e6;
+            if (cost < best) {
+                best = cost;
+                pick = GemmSlices{slices, i};
+            }
+        }
+    }
+    return pick;
+}
 
 void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile) {
     static constexpr int stages[kGemmConfigs] = {Gemm64::STAGES,   GemmMid::STAGES, GemmSmall::STAGES, GemmWide::STAGES,

@@ -94,11 +94,13 @@ struct GemmCfg {
 enum GemmOut {
     kOutF32,    // h, fp32
     kOutBf16,   // h rounded to bf16: gradients in their parameters' type
+    kOutPlanes, // h of one slice of K (blockIdx.y), fp32, to the slice's plane
     kOutGated,  // z = act(gate half of h) * up half of h, bf16, and h itself where it is wanted
 };
 struct GemmEpilogue {
     uint16_t *out16 = nullptr;  // bf16 h, or z
     int act = 0;                // kOutGated: the activation
+    int k_slice = 0;            // kOutPlanes: k of a slice, a multiple of 64
 };
 
 // (two wavefronts per SIMD at least: with 512 registers to a wavefront the compiler keeps the accumulators in
@@ -121,6 +123,15 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     int32_t *seg_c = seg_ad + 4 * BM;  // [BM] the buckets' indices (the token-order intermediate is addressed by them)
     int32_t *row_c = seg_c + BM;       // [BM] bucket per row (token-order form only; 0 where there is none)
 
+    const int pitch = d_in;  // of a row of x
+    if constexpr (OUT == kOutPlanes) {
+        const int k0 = (int)blockIdx.y * ep.k_slice;
+        x += k0;
+        W += (int64_t)k0 * d_out;
+        h += (int64_t)blockIdx.y * N * d_out;
+        d_in = min(ep.k_slice, d_in - k0);
+        if (blockIdx.y > 0) C = 0;  // the first slice takes the expand along
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
             if (slot_is_a(i)) {
                 const int k = T * BK + col * 8;
                 const int tok = tile_perm[row];
-                src = (k < d_in) ? x + (int64_t)(tok >= 0 ? tok : 0) * d_in + k : zero;
+                src = (k < d_in) ? x + (int64_t)(tok >= 0 ? tok : 0) * pitch + k : zero;
             } else {
                 const int k = T * BK + row;
                 src = (k < d_in) ? W + (int64_t)k * d_out + col : zero;
@@ -309,7 +320,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         int row, col;
         slot_geom(i, row, col);
         const int tok = tile_perm[row];
-        off_g[i] = (uint32_t)(((int64_t)(tok >= 0 ? tok : 0) * d_in + col * 8) * 2);
+        off_g[i] = (uint32_t)(((int64_t)(tok >= 0 ? tok : 0) * pitch + col * 8) * 2);
     }
 
     // `opaque` keeps the compiler from precomputing addresses (one per stage, k-step and fragment of

@@ -7,7 +7,7 @@ namespace {
 
 template <class Cfg, int OUT>
 hipError_t launch_out(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2, const int32_t *offsets,
-                      const int32_t *perm, float *h, int64_t N, int d_in, int d_out, int C, int rank, GemmEpilogue ep,
+                      const int32_t *perm, float *h, int64_t N, int d_in, int d_out, int C, int rank, GemmEpilogue ep, int slices,
                       hipStream_t s) {
     (void)&GemmKernel<Cfg, OUT>::lds;  // instantiates the registration
     const int tiles_m = (int)((N + Cfg::BM - 1) / Cfg::BM);
@@ -15,17 +15,16 @@ hipError_t launch_out(const uint16_t *x, const uint16_t *W, const uint16_t *B, c
     const int tiles_n = (cols + per - 1) / per;
     const unsigned blocks = (unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8);
     constexpr auto kernel = fused_gemm_kernel<Cfg, OUT>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
+    hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)slices), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
     return hipGetLastError();
 }
 
 template <int OUT>
-hipError_t launch_choice(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2, const int32_t *offsets,
-                         const int32_t *perm, float *h, int64_t N, int d_in, int d_out, int C, int rank, GemmEpilogue ep,
-                         hipStream_t s) {
-    if (N == 0) return hipSuccess;
-#define MOLORA_OUT_ARGS x, W, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, ep, s
-    switch (tiled_gemm_choice(N, d_in, d_out, C, rank)) {  // the order of kGemmCosts
+hipError_t launch_config(int config, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                         const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in, int d_out, int C, int rank,
+                         GemmEpilogue ep, int slices, hipStream_t s) {
+#define MOLORA_OUT_ARGS x, W, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, ep, slices, s
+    switch (config) {  // the order of kGemmCosts
         case 0: return launch_out<Gemm64, OUT>(MOLORA_OUT_ARGS);
         case 1: return launch_out<GemmMid, OUT>(MOLORA_OUT_ARGS);
         case 2: return launch_out<GemmSmall, OUT>(MOLORA_OUT_ARGS);
@@ -40,15 +39,25 @@ hipError_t launch_choice(const uint16_t *x, const uint16_t *W, const uint16_t *B
 }  // namespace
 
 hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
-                            const int32_t *offsets, const int32_t *perm, uint16_t *out, int64_t N, int d_in, int d_out,
-                            int C, int rank, hipStream_t s) {
-    return launch_choice<kOutBf16>(x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, GemmEpilogue{out, 0}, s);
+                            const int32_t *offsets, const int32_t *perm, uint16_t *out, float *planes, int64_t N, int d_in,
+                            int d_out, int C, int rank, hipStream_t s) {
+    if (N == 0) return hipSuccess;
+    const GemmSlices pick = sliced_gemm_choice(N, d_in, d_out, C, rank);
+    if (pick.slices == 1)
+        return launch_config<kOutBf16>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank,
+                                       GemmEpilogue{out}, 1, s);
+    const int k_slice = ((d_in + pick.slices - 1) / pick.slices + 63) / 64 * 64, slices = (d_in + k_slice - 1) / k_slice;
+    const hipError_t e = launch_config<kOutPlanes>(pick.config, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank,
+                                                   GemmEpilogue{nullptr, 0, k_slice}, slices, s);
+    return e != hipSuccess ? e : launch_sum_planes(planes, out, N * d_out, slices, s);
 }
 
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                              const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, int64_t N, int d_in,
                              int F, int C, int rank, int act, hipStream_t s) {
-    return launch_choice<kOutGated>(x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C, rank, GemmEpilogue{z, act}, s);
+    if (N == 0) return hipSuccess;
+    return launch_config<kOutGated>(tiled_gemm_choice(N, d_in, 2 * F, C, rank), x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C,
+                                    rank, GemmEpilogue{z, act}, 1, s);
 }
 
 }  // namespace molora
