@@ -26,10 +26,10 @@ __device__ __forceinline__ float gate_factor(float g, int act, float &slope) {
     }
     const float k = 1.5957691216057308f;  // 2 sqrt(2 / pi)
     const float y = act == MOLORA_ACT_SILU ? g : k * (g + 0.044715f * g * g * g);
-    const float p = 1.0f / (1.0f + __expf(-y));
+    const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-y));  // (a step of fp32 off at most)
     // (1 - p would lose what is left of p near 1: q is the same from the other side)
     if (SLOPE) {
-        const float q = 1.0f / (1.0f + __expf(y));
+        const float q = __builtin_amdgcn_rcpf(1.0f + __expf(y));
         const float d = p * q;
         slope = act == MOLORA_ACT_SILU ? d : d > 0.f ? d * k * (1.0f + 0.134145f * g * g) : 0.f;
     }

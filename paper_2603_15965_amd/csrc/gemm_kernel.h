@@ -693,33 +693,10 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         static_assert(EP_ROWS * EP_STRIDE <= STAGES * Cfg::STAGE, "epilogue staging fits the stages");
         static_assert(EP_ROWS * EP_CPR % NT == 0, "every thread stores the same number of chunks of a band");
         constexpr int EP_IT = EP_ROWS * EP_CPR / NT;
-        // A band of gate and up columns: h where it is wanted, and z, four columns to a thread.
-        auto gated_band = [&](int band) __attribute__((always_inline)) {
-            if (h != nullptr) {
-#pragma unroll
-                for (int j = 0; j < EP_IT; ++j) {
-                    const int it = tid + j * NT;
-                    const int r = it / EP_CPR, c = it % EP_CPR * 4, in = c % WCOLS;
-                    const int tok = tile_perm[(r >> 5) * (BM / Cfg::WM) + band * 32 + (r & 31)];
-                    const int col = n0 + c / WCOLS * (WCOLS / 2) + in % (WCOLS / 2);
-                    const f32x4 v = *(const f32x4 *)(smem + r * EP_STRIDE + c * 4);
-                    if (tok >= 0 && col < half_out)
-                        __builtin_nontemporal_store(v, (f32x4 *)(h + (int64_t)tok * d_out + col + (in >= WCOLS / 2 ? half_out : 0)));
-                }
-            }
-#pragma unroll
-            for (int it = tid; it < EP_ROWS * EP_CPR / 2; it += NT) {
-                const int r = it / (EP_CPR / 2), c = it % (EP_CPR / 2) * 4;
-                const int at = c / (WCOLS / 2) * WCOLS + c % (WCOLS / 2);  // in the tile
-                const int tok = tile_perm[(r >> 5) * (BM / Cfg::WM) + band * 32 + (r & 31)];
-                const f32x4 g = *(const f32x4 *)(smem + r * EP_STRIDE + at * 4);
-                const f32x4 u = *(const f32x4 *)(smem + r * EP_STRIDE + (at + WCOLS / 2) * 4);
-                if (tok >= 0 && n0 + c < half_out)
-                    __builtin_nontemporal_store(bf16x4_bits(gate4(g, u, ep.act)), (u32x2 *)(ep.out16 + (int64_t)tok * half_out + n0 + c));
-            }
-        };
+        const bool store_h = !GATED || h != nullptr;
 #pragma unroll
         for (int band = 0; band < TM / 2; ++band) {
+            if (!store_h) break;
             __syncthreads();  // operand stages (or the previous band) are no longer read
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -727,10 +704,6 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
                 for (int tn = 0; tn < TN; ++tn)
                     *(f32x4 *)(smem + (wm * 32 + i * 16 + l16) * EP_STRIDE + (wn * (BN / Cfg::WN) + tn * 16 + kg * 4) * 4) = acc[band * 2 + i][tn];
             __syncthreads();
-            if constexpr (GATED) {
-                gated_band(band);
-                continue;
-            }
             // All of a thread's staged chunks and their rows' tokens are read before the first
             // store is issued: as a loop that reads one token, waits, reads one chunk, waits and
             // stores, the band took two LDS round trips per chunk, eight chunks in a row.
@@ -747,13 +720,45 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
 #pragma unroll
             for (int j = 0; j < EP_IT; ++j) {
                 const int col = n0 + ((tid + j * NT) % EP_CPR) * 4;
-                if constexpr (OUT == kOutBf16) {
+                if constexpr (GATED) {
+                    const int c = (tid + j * NT) % EP_CPR * 4, in = c % WCOLS, at = n0 + c / WCOLS * (WCOLS / 2) + in % (WCOLS / 2);
+                    if (tok[j] >= 0 && at < half_out)
+                        __builtin_nontemporal_store(val[j], (f32x4 *)(h + (int64_t)tok[j] * d_out + at + (in >= WCOLS / 2 ? half_out : 0)));
+                } else if constexpr (OUT == kOutBf16) {
                     if (tok[j] >= 0 && col < d_out)
                         __builtin_nontemporal_store(bf16x4_bits(val[j]), (u32x2 *)(ep.out16 + (int64_t)tok[j] * d_out + col));
                 } else if (tok[j] >= 0 && col < d_out)
                     // h is written once and not read again here: a streaming store keeps it
                     // from displacing x and W tiles in L2 (measured: -11 % at config 1)
                     __builtin_nontemporal_store(val[j], (f32x4 *)(h + (int64_t)tok[j] * d_out + col));
+            }
+        }
+        if constexpr (GATED) {
+            // z in registers, where a lane holds both factors, then the whole tile through LDS in bf16, so that a
+            // store covers 16 bytes of a row's BN contiguous ones
+            constexpr int Z_STRIDE = BN + 16, Z_CPR = BN / 16, Z_IT = BM * Z_CPR / NT;
+            static_assert(BM * Z_STRIDE <= STAGES * Cfg::STAGE && BM * Z_CPR % NT == 0, "z fits the stages");
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int tn = 0; tn < TN / 2; ++tn)
+                    *(u32x2 *)(smem + (wm * (BM / Cfg::WM) + i * 16 + l16) * Z_STRIDE + (wn * (WCOLS / 2) + tn * 16 + kg * 4) * 2) =
+                        bf16x4_bits(gate4(acc[i][tn], acc[i][tn + TN / 2], ep.act));
+            __syncthreads();
+            int tok[Z_IT];
+            u32x4 val[Z_IT];
+#pragma unroll
+            for (int j = 0; j < Z_IT; ++j) {
+                const int it = tid + j * NT;
+                tok[j] = tile_perm[it / Z_CPR];
+                val[j] = *(const u32x4 *)(smem + it / Z_CPR * Z_STRIDE + it % Z_CPR * 16);
+            }
+#pragma unroll
+            for (int j = 0; j < Z_IT; ++j) {
+                const int col = n0 + (tid + j * NT) % Z_CPR * 8;
+                if (tok[j] >= 0 && col < half_out)
+                    __builtin_nontemporal_store(val[j], (u32x4 *)(ep.out16 + (int64_t)tok[j] * half_out + col));
             }
         }
     }
