@@ -76,7 +76,7 @@ inline bool adapters_given(const void *A, const void *B, const int32_t *r, int32
 struct GatedWorkspace {
     int32_t *offsets, *perm;
     uint16_t *t2;
-    float *base, *planes;  // at most 64 tokens: x W, in slices of K
+    float *base, *planes;  // at most 64 tokens: x W, in slices of K; more: fp32 sums where the GEMM does not end in z
     int slices;
     size_t bytes;
 };
@@ -93,6 +93,8 @@ inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F
         w.slices = molora::small_base_slices(N, d_in, 2 * F, C);
         w.base = c.take<float>(plane);
         if (w.slices > 1) w.planes = c.take<float>(plane * (w.slices - 1));
+    } else {
+        w.planes = c.take<float>(size_t(molora::gemm_plane_floats(N, 2 * int64_t(F))) * 4);
     }
     w.bytes = c.at;
     return w;
@@ -271,7 +273,7 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
         return from_hip(molora::launch_gated_finish(base, w.planes, w.slices, Bb, r, w.t2, w.perm, zb, pre, N, F, C, rank, act, s));
     }
     if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
-    return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, N, d_in, F, C, rank, act, s));
+    return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, w.planes, N, d_in, F, C, rank, act, s));
 }
 
 size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {

@@ -183,8 +183,7 @@ void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile
 
 // ---- the fused GEMM with other outputs (gemm_out.hip); offsets, perm and t2 as launch_fused_gemm, or perm == nullptr and
 // C = 0: rows in order, without adapters.  Operands below 4 GiB each (fused_gemm_sizes_ok with a tile forced). ----
-// out = x W + t B_c in bf16.  planes: scratch of gemm_plane_floats(N, d_out) floats, for K in slices where the output has
-// too few tiles for the chip
+// out = x W + t B_c in bf16.  planes: scratch of gemm_plane_floats(N, d_out) floats (sliced_gemm_choice)
 constexpr int kMaxGemmSlices = 8;
 constexpr int64_t kMaxPlaneFloats = int64_t(8) << 20;
 inline int64_t gemm_plane_floats(int64_t N, int64_t d_out) {
@@ -195,13 +194,13 @@ hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t
                             const int32_t *offsets, const int32_t *perm, uint16_t *out, float *planes, int64_t N, int d_in,
                             int d_out, int C, int rank, hipStream_t s);
 struct GemmSlices {
-    int slices, config;
+    int slices, config;  // config -1: the streaming kernel
 };
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
-// h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr
+// h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr; planes as above
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
-                             const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, int64_t N, int d_in,
-                             int F, int C, int rank, int act, hipStream_t s);
+                             const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, float *planes, int64_t N,
+                             int d_in, int F, int C, int rank, int act, hipStream_t s);
 // the tile configuration that the cost rule takes where the streaming kernel is not to be had
 int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
 
@@ -211,6 +210,8 @@ int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
 hipError_t launch_gated_finish(const float *base, const float *planes, int slices, const uint16_t *B, const int32_t *r,
                                const uint16_t *t2, const int32_t *perm, uint16_t *z, float *pre, int64_t N, int F, int C, int rank,
                                int act, hipStream_t s);
+// h = the sum of `count` planes [N][2 F], z from it, h stored where pre != nullptr
+hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, int64_t N, int F, int act, hipStream_t s);
 // dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F]; rows N .. padded - 1 are zero
 hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
                                 int act, hipStream_t s);

@@ -10,8 +10,28 @@ namespace {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 
-// One thread takes four columns of a row.
-// dh is rounded to bf16 here: it is an operand of the matrix instructions in every gradient that follows.  (h comes
+// The activation and the product by themselves, where the projection leaves fp32 sums.  One thread takes four columns.
+__global__ __launch_bounds__(256) void gate_kernel(const float *planes, int count, uint16_t *__restrict__ z, float *pre, int64_t items,
+                                                   int F, int act) {
+    const int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (it >= items) return;
+    const int per = F / 4;
+    const int64_t row = it / per, all = items * 8;  // floats of a plane
+    const int col = (int)(it % per) * 4;
+    const int64_t at = row * 2 * F + col;
+    f32x4 g = *(const f32x4 *)(planes + at), u = *(const f32x4 *)(planes + at + F);
+    for (int i = 1; i < count; ++i) {
+        g += *(const f32x4 *)(planes + i * all + at);
+        u += *(const f32x4 *)(planes + i * all + at + F);
+    }
+    if (pre != nullptr) {
+        *(f32x4 *)(pre + at) = g;
+        *(f32x4 *)(pre + at + F) = u;
+    }
+    *(u32x2 *)(z + row * F + col) = bf16x4_bits(gate4(g, u, act));
+}
+
+// One thread takes four columns of a row.  dh is rounded to bf16 here: it is an operand of the matrix instructions in every gradient that follows.  (h comes
 // in fp32: with g and u rounded too, the gradients would be 1.9 instead of 1.4 times as far from their exact
 // values as their own rounding to bf16 puts them.)
 __global__ __launch_bounds__(256) void gate_backward_kernel(const uint16_t *__restrict__ dz, const float *__restrict__ pre,
@@ -235,6 +255,13 @@ hipError_t launch_zero(void *dst, int64_t bytes, hipStream_t s) {
     const int64_t n = bytes / 16, blocks = (n + 255) / 256;
     if (n > 0)
         hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, (u32x4 *)dst, n);
+    return hipGetLastError();
+}
+
+hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, int64_t N, int F, int act, hipStream_t s) {
+    const int64_t items = N * (F / 4), blocks = (items + 255) / 256;
+    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+    if (blocks > 0) hipLaunchKernelGGL(gate_kernel, dim3((unsigned)blocks), dim3(256), 0, s, planes, count, z, pre, items, F, act);
     return hipGetLastError();
 }
 

@@ -113,16 +113,25 @@ int gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming = t
 
 int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) { return gemm_choice(N, d_in, d_out, C, R, false); }
 
-// The same with K in slices: their sums cost a second launch and a trip through memory.
+// The cheapest way to an output that is not h itself: one launch that ends in it, or fp32 sums in memory, of the
+// streaming kernel (many wide adapters against a small batch: its expand is the cheaper one) or of K in slices (few
+// output tiles, long K), and a second launch that ends them.
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) {
     GemmSlices pick{1, gemm_choice(N, d_in, d_out, C, R, false)};
     double best = tiled_cost(kGemmCosts[pick.config], N, d_in, d_out, C, R);
+    const double floats = (double)N * d_out;
+    const auto second = [&](int slices) { return 4.0 + slices * floats * 8 / 4e6; };  // (4 MB a microsecond, written and read)
+    if (N <= kSmallBatchMax && floats <= (double)kMaxPlaneFloats) {
+        const double cost = streaming_cost(N, d_in, d_out, C, R) + second(1);
+        if (cost < best) {
+            best = cost;
+            pick = GemmSlices{1, -1};
+        }
+    }
     for (int slices = 2; slices <= kMaxGemmSlices; ++slices) {
-        const double floats = (double)slices * (double)N * d_out;
-        if (floats > (double)kMaxPlaneFloats || d_in < slices * 256) break;
+        if (slices * floats > (double)kMaxPlaneFloats || d_in < slices * 256) break;
         for (int i = 0; i < kGemmConfigs; ++i) {
-            // (4 MB a microsecond written and read, and the launch)
-            const double cost = tiled_cost(kGemmCosts[i], N, d_in, d_out, C, R, slices) + 4.0 + floats * 8 / 4e6;
+            const double cost = tiled_cost(kGemmCosts[i], N, d_in, d_out, C, R, slices) + second(slices);
             if (cost < best) {
                 best = cost;
                 pick = GemmSlices{slices, i};

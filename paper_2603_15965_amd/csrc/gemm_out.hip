@@ -38,26 +38,45 @@ hipError_t launch_config(int config, const uint16_t *x, const uint16_t *W, const
 
 }  // namespace
 
+namespace {
+// fp32 sums of x W + t B_c to planes, `count` of them
+hipError_t launch_planes(const GemmSlices &pick, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                         const int32_t *offsets, const int32_t *perm, float *planes, int64_t N, int d_in, int d_out, int C,
+                         int rank, int &count, hipStream_t s) {
+    count = 1;
+    if (pick.config < 0) return launch_small_batch_gemm(x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, Mix{1, C, nullptr, nullptr}, s);
+    const int k_slice = ((d_in + pick.slices - 1) / pick.slices + 63) / 64 * 64;
+    count = (d_in + k_slice - 1) / k_slice;
+    return launch_config<kOutPlanes>(pick.config, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank,
+                                     GemmEpilogue{nullptr, 0, k_slice}, count, s);
+}
+}  // namespace
+
 hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                             const int32_t *offsets, const int32_t *perm, uint16_t *out, float *planes, int64_t N, int d_in,
                             int d_out, int C, int rank, hipStream_t s) {
     if (N == 0) return hipSuccess;
-    const GemmSlices pick = sliced_gemm_choice(N, d_in, d_out, C, rank);
-    if (pick.slices == 1)
+    GemmSlices pick = sliced_gemm_choice(N, d_in, d_out, C, rank);
+    if (perm == nullptr && pick.config < 0) pick = GemmSlices{1, tiled_gemm_choice(N, d_in, d_out, C, rank)};  // it wants a dispatch
+    if (pick.slices == 1 && pick.config >= 0)
         return launch_config<kOutBf16>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank,
                                        GemmEpilogue{out}, 1, s);
-    const int k_slice = ((d_in + pick.slices - 1) / pick.slices + 63) / 64 * 64, slices = (d_in + k_slice - 1) / k_slice;
-    const hipError_t e = launch_config<kOutPlanes>(pick.config, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank,
-                                                   GemmEpilogue{nullptr, 0, k_slice}, slices, s);
-    return e != hipSuccess ? e : launch_sum_planes(planes, out, N * d_out, slices, s);
+    int count;
+    const hipError_t e = launch_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, count, s);
+    return e != hipSuccess ? e : launch_sum_planes(planes, out, N * d_out, count, s);
 }
 
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
-                             const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, int64_t N, int d_in,
-                             int F, int C, int rank, int act, hipStream_t s) {
+                             const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, float *planes, int64_t N,
+                             int d_in, int F, int C, int rank, int act, hipStream_t s) {
     if (N == 0) return hipSuccess;
-    return launch_config<kOutGated>(tiled_gemm_choice(N, d_in, 2 * F, C, rank), x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C,
-                                    rank, GemmEpilogue{z, act}, 1, s);
+    GemmSlices pick = sliced_gemm_choice(N, d_in, 2 * F, C, rank);
+    if (perm == nullptr && pick.config < 0) pick = GemmSlices{1, tiled_gemm_choice(N, d_in, 2 * F, C, rank)};
+    if (pick.slices == 1 && pick.config >= 0)
+        return launch_config<kOutGated>(pick.config, x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C, rank, GemmEpilogue{z, act}, 1, s);
+    int count;
+    const hipError_t e = launch_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, count, s);
+    return e != hipSuccess ? e : launch_gate(planes, count, z, pre, N, F, act, s);
 }
 
 }  // namespace molora
