@@ -26,6 +26,15 @@ inline bool mx_product_ok(int64_t N, int32_t d_in, int32_t d_out) {
 
 constexpr int64_t kDecode = 64;  // batches that are one read of the base weight
 
+// Scratch of a shrink of any batch of up to N tokens (it does not grow with the batch).
+inline size_t shrink_scratch_up_to(int64_t N, int32_t d_in, int32_t C, int32_t rank) {
+    int64_t peaks[molora::kShrinkPeaks];
+    const int n = molora::shrink_scratch_peaks(N, d_in, C, rank, peaks);
+    size_t most = molora::shrink_scratch_bytes(N, d_in, C, rank);
+    for (int i = 0; i < n; ++i) most = std::max(most, molora::shrink_scratch_bytes(peaks[i], d_in, C, rank));
+    return most;
+}
+
 struct Cutter {  // pieces of a workspace, each 256-byte aligned
     unsigned char *base;
     size_t at = 0;
@@ -42,7 +51,7 @@ struct MxWorkspace {
     int32_t *offsets, *perm;
     uint16_t *t2;
     uint8_t *codes, *scales;
-    float *planes;  // at most 64 tokens: x A_r in slices of K
+    float *planes;  // x A_r in slices of K
     size_t bytes;
 };
 inline MxWorkspace carve_mx(void *base, int64_t N, int32_t d_in, int32_t C, int32_t rank) {
@@ -56,6 +65,7 @@ inline MxWorkspace carve_mx(void *base, int64_t N, int32_t d_in, int32_t C, int3
         w.offsets = c.take<int32_t>(size_t(C + 1) * 4);
         w.perm = c.take<int32_t>(size_t(N) * 4);
         w.t2 = c.take<uint16_t>(size_t(N) * 2 * rank * 2);
+        w.planes = c.take<float>(shrink_scratch_up_to(N, d_in, C, rank));
     }
     w.bytes = c.at;
     return w;
@@ -94,7 +104,9 @@ inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F
         w.base = c.take<float>(plane);
         if (w.slices > 1) w.planes = c.take<float>(plane * (w.slices - 1));
     } else {
-        w.planes = c.take<float>(size_t(molora::gemm_plane_floats(N, 2 * int64_t(F))) * 4);
+        size_t bytes = size_t(molora::gemm_plane_floats(N, 2 * int64_t(F))) * 4;
+        if (C > 0) bytes = std::max(bytes, shrink_scratch_up_to(N, d_in, C, rank));
+        w.planes = c.take<float>(bytes);
     }
     w.bytes = c.at;
     return w;
@@ -131,11 +143,14 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
     w.dh = c.take<uint16_t>(size_t(padded_rows(N)) * 2 * F * 2);
     w.xt = c.take<uint16_t>(size_t(padded_rows(N)) * d_in * 2);
     w.wt = c.take<uint16_t>(size_t(d_in) * 2 * F * 2);
-    // fp32 sums of one product at a time: slices of K of dx and dW, pieces of the rows of dA and dB
+    // fp32 sums of one product at a time: slices of K of t, s, dx and dW, pieces of the rows of dA and dB
     size_t floats = size_t(molora::gemm_plane_floats(N, d_in));
     floats = std::max(floats, size_t(molora::gemm_plane_floats(d_in, 2 * int64_t(F))));
     w.outer_a = C > 0 ? round256(molora::grouped_outer_floats(N, d_in, C, rank) * 4) / 4 : 0;
-    if (C > 0) floats = std::max(floats, w.outer_a + molora::grouped_outer_floats(N, 2 * F, C, rank));
+    if (C > 0) {
+        floats = std::max(floats, w.outer_a + molora::grouped_outer_floats(N, 2 * F, C, rank));
+        floats = std::max(floats, std::max(shrink_scratch_up_to(N, d_in, C, rank), shrink_scratch_up_to(N, 2 * F, C, rank)) / 4);
+    }
     w.planes = c.take<float>(floats * 4);
     w.bytes = c.at;
     return w;
@@ -143,7 +158,8 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
 
 // The dispatch step and t = x A_c of a batch of more than 64 tokens: one launch where that pays, as in molora_apply.
 inline hipError_t dispatch_shrink(const int32_t *r, const uint16_t *x, const uint16_t *A, int32_t *offsets, int32_t *perm,
-                                  uint16_t *t2, int64_t N, int32_t d_in, int32_t C, int32_t rank, hipStream_t s) {
+                                  uint16_t *t2, float *scratch, int64_t N, int32_t d_in, int32_t C, int32_t rank,
+                                  hipStream_t s) {
     const molora::Mix plain{1, C, nullptr, nullptr};
     molora::SortArgs sort;
     if (molora::sort_large_in_shrink(N, d_in, C, rank)) {
@@ -152,7 +168,7 @@ inline hipError_t dispatch_shrink(const int32_t *r, const uint16_t *x, const uin
         const hipError_t e = molora::launch_bucket(r, offsets, perm, N, C, nullptr, s);
         if (e != hipSuccess) return e;
     }
-    return molora::launch_shrink(x, A, offsets, perm, t2, N, d_in, C, rank, plain, s, nullptr, sort);
+    return molora::launch_shrink(x, A, offsets, perm, t2, N, d_in, C, rank, plain, s, scratch, sort);
 }
 
 #define MOLORA_TRY(call)                              \
@@ -238,7 +254,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
         MOLORA_TRY(molora::launch_mx_decode_first(xb, Ab, r, w.codes, w.scales, w.planes, N, d_in, C, rank, s));
         return from_hip(molora::launch_mx_decode(w.codes, w.scales, wcb, wsb, Bb, r, w.planes, h, N, d_in, d_out, C, rank, s));
     }
-    MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
+    MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));
     MOLORA_TRY(molora::launch_mx_quantize(x, false, w.perm, w.codes, w.scales, N, d_in, s));
     return from_hip(molora::launch_mx_gemm(w.codes, w.scales, wcb, wsb, Bb, w.t2, w.offsets, w.perm, h, N, d_in, d_out, C, rank, s));
 }
@@ -272,7 +288,7 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
                                                     molora::SortArgs{r, w.offsets, w.perm, nullptr}, s, false, w.planes, w.slices));
         return from_hip(molora::launch_gated_finish(base, w.planes, w.slices, Bb, r, w.t2, w.perm, zb, pre, N, F, C, rank, act, s));
     }
-    if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
+    if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));
     return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, w.planes, N, d_in, F, C, rank, act, s));
 }
 
@@ -317,12 +333,12 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
     MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
     if (C > 0) {
         if (dB && N > kDecode)
-            MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, s));
+            MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));
         else
             MOLORA_TRY(molora::launch_bucket(r, w.offsets, w.perm, N, C, nullptr, s));
-        if (dB && N <= kDecode) MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s));
+        if (dB && N <= kDecode) MOLORA_TRY(molora::launch_shrink(xb, Ab, w.offsets, w.perm, w.t2, N, d_in, C, rank, plain, s, w.planes));
         if (dx || dA)  // s = dh B^T
-            MOLORA_TRY(molora::launch_shrink(w.dh, w.bt, w.offsets, w.perm, w.s2, N, 2 * F, C, rank, plain, s));
+            MOLORA_TRY(molora::launch_shrink(w.dh, w.bt, w.offsets, w.perm, w.s2, N, 2 * F, C, rank, plain, s, w.planes));
         molora::GroupedOuter outer[2];
         int outers = 0;
         if (dA) outer[outers++] = {xb, w.s2, static_cast<uint16_t *>(dA), w.planes, d_in, false};

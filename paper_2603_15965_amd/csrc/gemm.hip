@@ -78,7 +78,7 @@ double tiled_cost(const GemmCost &g, int64_t N, int d_in, int d_out, int C, int 
     const double last = (double)(tiles % slots) / (double)slots, part = last > 0 ? 1 : 0;
     const double kt = (d_in + 64 * slices - 1) / (64 * slices);
     const double segs = fmin((double)C, 1.0 + (double)g.bm * C / (double)N);  // buckets that own rows of a tile
-    const double expand = segs * ((R + 15) / 16) / 4 + (R + 31) / 32;
+    const double expand = segs / slices * ((R + 15) / 16) / 4 + (R + 31) / 32;
     return g.once + g.per_round * (double)full + g.partial * part + kt * (g.k_round * (double)full + g.k_few * part + g.k_full * last) +
            g.expand * ((double)full + part) * expand;
 }

@@ -130,7 +130,6 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         W += (int64_t)k0 * d_out;
         h += (int64_t)blockIdx.y * N * d_out;
         d_in = min(ep.k_slice, d_in - k0);
-        if (blockIdx.y > 0) C = 0;  // the first slice takes the expand along
     }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -294,7 +293,9 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         // does one of the tile's blocks hold rows of the bucket?  (blocks are counted in steps from
         // blk0; the first one that ends after the bucket's first row)
         const int k = max(0, (o_lo - blk0 - 31 + blk_step - 1) / blk_step);
-        if (o_lo < o_hi && k < BM / 32 && blk_pos(k) < o_hi) {
+        bool mine = true;
+        if constexpr (OUT == kOutPlanes) mine = c % (int)gridDim.y == (int)blockIdx.y;  // the slices share the buckets' expand
+        if (mine && o_lo < o_hi && k < BM / 32 && blk_pos(k) < o_hi) {
             const int idx = atomicAdd(nseg_p, 1);
             seg_lo[idx] = o_lo;
             seg_hi[idx] = o_hi;
