@@ -694,7 +694,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         static_assert(EP_ROWS * EP_STRIDE <= STAGES * Cfg::STAGE, "epilogue staging fits the stages");
         static_assert(EP_ROWS * EP_CPR % NT == 0, "every thread stores the same number of chunks of a band");
         constexpr int EP_IT = EP_ROWS * EP_CPR / NT;
-        const bool store_h = !GATED || h != nullptr;
+        const bool store_h = OUT == kOutF32 || OUT == kOutPlanes || (GATED && h != nullptr);
 #pragma unroll
         for (int band = 0; band < TM / 2; ++band) {
             if (!store_h) break;
@@ -703,7 +703,11 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int tn = 0; tn < TN; ++tn)
-                    *(f32x4 *)(smem + (wm * 32 + i * 16 + l16) * EP_STRIDE + (wn * (BN / Cfg::WN) + tn * 16 + kg * 4) * 4) = acc[band * 2 + i][tn];
+                {
+                    // (the gated tile's halves one after the other: BN * 2 contiguous bytes of a row of h each)
+                    const int c = GATED ? (tn < TN / 2 ? 0 : BN / 2) + wn * (WCOLS / 2) + tn % (TN / 2) * 16 : wn * (BN / Cfg::WN) + tn * 16;
+                    *(f32x4 *)(smem + (wm * 32 + i * 16 + l16) * EP_STRIDE + (c + kg * 4) * 4) = acc[band * 2 + i][tn];
+                }
             __syncthreads();
             // All of a thread's staged chunks and their rows' tokens are read before the first
             // store is issued: as a loop that reads one token, waits, reads one chunk, waits and
@@ -722,44 +726,48 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
             for (int j = 0; j < EP_IT; ++j) {
                 const int col = n0 + ((tid + j * NT) % EP_CPR) * 4;
                 if constexpr (GATED) {
-                    const int c = (tid + j * NT) % EP_CPR * 4, in = c % WCOLS, at = n0 + c / WCOLS * (WCOLS / 2) + in % (WCOLS / 2);
+                    const int c = (tid + j * NT) % EP_CPR * 4, up = c >= BN / 2 ? 1 : 0, at = n0 + c - up * (BN / 2);
                     if (tok[j] >= 0 && at < half_out)
-                        __builtin_nontemporal_store(val[j], (f32x4 *)(h + (int64_t)tok[j] * d_out + at + (in >= WCOLS / 2 ? half_out : 0)));
-                } else if constexpr (OUT == kOutBf16) {
-                    if (tok[j] >= 0 && col < d_out)
-                        __builtin_nontemporal_store(bf16x4_bits(val[j]), (u32x2 *)(ep.out16 + (int64_t)tok[j] * d_out + col));
+                        __builtin_nontemporal_store(val[j], (f32x4 *)(h + (int64_t)tok[j] * d_out + at + up * half_out));
                 } else if (tok[j] >= 0 && col < d_out)
                     // h is written once and not read again here: a streaming store keeps it
                     // from displacing x and W tiles in L2 (measured: -11 % at config 1)
                     __builtin_nontemporal_store(val[j], (f32x4 *)(h + (int64_t)tok[j] * d_out + col));
             }
         }
-        if constexpr (GATED) {
-            // z in registers, where a lane holds both factors, then the whole tile through LDS in bf16, so that a
-            // store covers 16 bytes of a row's BN contiguous ones
-            constexpr int Z_STRIDE = BN + 16, Z_CPR = BN / 16, Z_IT = BM * Z_CPR / NT;
-            static_assert(BM * Z_STRIDE <= STAGES * Cfg::STAGE && BM * Z_CPR % NT == 0, "z fits the stages");
-            __syncthreads();
+        if constexpr (GATED || OUT == kOutBf16) {
+            // bf16 through LDS, so that a store covers 16 bytes of a row's contiguous ones: z, made in registers, where a
+            // lane holds both factors, or h; the rows of a half of every wavefront's tiles at a time
+            constexpr int COLS = GATED ? BN / 2 : BN, WC = COLS / Cfg::WN, TN16 = GATED ? TN / 2 : TN;
+            constexpr int ROWS = BM / 2, WR = ROWS / Cfg::WM, STRIDE = COLS * 2 + 16, CPR = COLS / 8, IT = ROWS * CPR / NT;
+            static_assert(ROWS * STRIDE <= STAGES * Cfg::STAGE && ROWS * CPR % NT == 0, "half a tile fits the stages");
+            const int out_cols = GATED ? half_out : d_out;
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int half = 0; half < 2; ++half) {
+                __syncthreads();
 #pragma unroll
-                for (int tn = 0; tn < TN / 2; ++tn)
-                    *(u32x2 *)(smem + (wm * (BM / Cfg::WM) + i * 16 + l16) * Z_STRIDE + (wn * (WCOLS / 2) + tn * 16 + kg * 4) * 2) =
-                        bf16x4_bits(gate4(acc[i][tn], acc[i][tn + TN / 2], ep.act));
-            __syncthreads();
-            int tok[Z_IT];
-            u32x4 val[Z_IT];
+                for (int i = 0; i < TM / 2; ++i)
 #pragma unroll
-            for (int j = 0; j < Z_IT; ++j) {
-                const int it = tid + j * NT;
-                tok[j] = tile_perm[it / Z_CPR];
-                val[j] = *(const u32x4 *)(smem + it / Z_CPR * Z_STRIDE + it % Z_CPR * 16);
-            }
+                    for (int tn = 0; tn < TN16; ++tn) {
+                        f32x4 v = acc[half * (TM / 2) + i][tn];
+                        if constexpr (GATED) v = gate4(v, acc[half * (TM / 2) + i][tn + TN / 2], ep.act);
+                        *(u32x2 *)(smem + (wm * WR + i * 16 + l16) * STRIDE + (wn * WC + tn * 16 + kg * 4) * 2) = bf16x4_bits(v);
+                    }
+                __syncthreads();
+                int tok[IT];
+                u32x4 val[IT];
 #pragma unroll
-            for (int j = 0; j < Z_IT; ++j) {
-                const int col = n0 + (tid + j * NT) % Z_CPR * 8;
-                if (tok[j] >= 0 && col < half_out)
-                    __builtin_nontemporal_store(val[j], (u32x4 *)(ep.out16 + (int64_t)tok[j] * half_out + col));
+                for (int j = 0; j < IT; ++j) {
+                    const int it = tid + j * NT, r = it / CPR;
+                    tok[j] = tile_perm[r / WR * (BM / Cfg::WM) + half * WR + r % WR];
+                    val[j] = *(const u32x4 *)(smem + r * STRIDE + it % CPR * 16);
+                }
+#pragma unroll
+                for (int j = 0; j < IT; ++j) {
+                    const int col = n0 + (tid + j * NT) % CPR * 8;
+                    if (tok[j] >= 0 && col < out_cols)
+                        __builtin_nontemporal_store(val[j], (u32x4 *)(ep.out16 + (int64_t)tok[j] * out_cols + col));
+                }
             }
         }
     }
