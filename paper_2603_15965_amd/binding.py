@@ -785,8 +785,17 @@ def molora_mx_matmul(xc, xs, wc, ws, N, d_in, d_out, h=None, stream=None):
     return h
 
 
-def _bytes(fn, *sizes):
-    return int(getattr(load(), fn)(*sizes))
+def _workspace(fn, sizes, workspace, device, stream):
+    """The caller's workspace, or one for this call: from the memory of the stream that the call runs on, so that
+    what is given back at its end is not handed to another stream while the kernels still use it."""
+    if workspace is None:
+        nbytes = max(int(getattr(_lib or load(), fn)(*sizes)), 256)
+        if stream is None:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _flat_bytes(workspace, "workspace")
 
 
 def molora_apply_mx(x, wc, ws, A, B, r, h=None, workspace=None, stream=None):
@@ -796,11 +805,8 @@ def molora_apply_mx(x, wc, ws, A, B, r, h=None, workspace=None, stream=None):
     d_out = _three(B, "B")[2]
     if h is None:
         h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
-    if workspace is None:
-        nbytes = _bytes("molora_apply_mx_workspace_bytes", N, d_in, d_out, C, rank)
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=x.device)
     bf = torch.bfloat16
-    work, work_bytes = _flat_bytes(workspace, "workspace")
+    work, work_bytes = _workspace("molora_apply_mx_workspace_bytes", (N, d_in, d_out, C, rank), workspace, x.device, stream)
     _call_here("molora_apply_mx", _dev(x, bf, "x"), *_mx(wc, ws, d_out, d_in, "W"), _dev(A, bf, "A", (C, d_in, rank)),
           _dev(B, bf, "B", (C, rank, d_out)), _dev(r, torch.int32, "r", (N,)), _dev(h, torch.float32, "h", (N, d_out)),
           N, d_in, d_out, C, rank, work, work_bytes, _stream(stream))
@@ -828,12 +834,6 @@ def _gated_args(x, W, A, B, r, act):
     return ops, (N, d_in, wide // 2, C, rank), _ACTS[act]
 
 
-def _gated_workspace(fn, sizes, workspace, device):
-    if workspace is None:
-        workspace = torch.empty(max(_bytes(fn, *sizes), 256), dtype=torch.uint8, device=device)
-    return _flat_bytes(workspace, "workspace")
-
-
 def molora_apply_gated(x, W, A=None, B=None, r=None, act="silu", z=None, pre=None, workspace=None, stream=None):
     """z = act(h[:, :F]) * h[:, F:] (bf16 [N][F]) with h = x W + (x A[r]) B[r] of 2 F columns, gate and
     up side by side.  pre (fp32 [N][2 F]): filled with h, which molora_gated_backward takes.  act: "silu",
@@ -842,7 +842,7 @@ def molora_apply_gated(x, W, A=None, B=None, r=None, act="silu", z=None, pre=Non
     N, F = sizes[0], sizes[2]
     if z is None:
         z = torch.empty((N, F), dtype=torch.bfloat16, device=x.device)
-    work, work_bytes = _gated_workspace("molora_apply_gated_workspace_bytes", sizes, workspace, x.device)
+    work, work_bytes = _workspace("molora_apply_gated_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_apply_gated", *ops, _dev(z, torch.bfloat16, "z", (N, F)), _opt(pre, torch.float32, "pre", (N, 2 * F)), *sizes, code,
           work, work_bytes, _stream(stream))
     return z
@@ -868,7 +868,7 @@ def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A
         if t is None:
             t = torch.empty(shape, dtype=bf, device=x.device)
         out.append((t, _dev(t, bf, f"d{name}", shape)))
-    work, work_bytes = _gated_workspace("molora_gated_backward_workspace_bytes", sizes, workspace, x.device)
+    work, work_bytes = _workspace("molora_gated_backward_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_gated_backward", _dev(dz, bf, "dz", (N, F)), *ops, _dev(pre, torch.float32, "pre", (N, 2 * F)), *(d for _, d in out),
           *sizes, code, work, work_bytes, _stream(stream))
     return tuple(t for t, _ in out)

@@ -222,3 +222,31 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     with pytest.raises(ValueError, match="the current device is cuda:1"):
         mb.molora_mx_quantize(args[0])
     assert bool((z == 7).all())
+
+
+def test_another_stream_and_workspaces_of_the_calls_own():
+    """Calls on a side stream that allocate their workspaces, while the default stream allocates and fills memory of
+    the same size: nothing of what the side stream still uses may be handed out."""
+    torch, mb = _gpu()
+    N, d, F, C, rank = 300, 264, 520, 4, 16
+    w, r, dzb = _case(N, d, F, C, rank)
+    args = _tensors(torch, mb, w, r, C)
+    dz = mb.bf16_tensor(dzb)
+    wc, ws = mb.molora_mx_quantize_w(args[1])
+    pre = torch.empty(N, 2 * F, dtype=torch.float32, device="cuda")
+    z = mb.molora_apply_gated(*args, pre=pre)
+    want = (z, *mb.molora_gated_backward(dz, *args, pre), mb.molora_apply_mx(args[0], wc, ws, *args[2:]))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    sizes = [int(f(N, d, F, C, rank)) for f in (mb.load().molora_apply_gated_workspace_bytes, mb.load().molora_gated_backward_workspace_bytes)]
+    for handle in (side, side.cuda_stream):
+        for _ in range(3):
+            outs = [torch.empty_like(t) for t in want]
+            torch.cuda.synchronize()
+            mb.molora_apply_gated(*args, z=outs[0], stream=handle)
+            mb.molora_gated_backward(dz, *args, pre, dx=outs[1], dW=outs[2], dA=outs[3], dB=outs[4], stream=handle)
+            mb.molora_apply_mx(args[0], wc, ws, *args[2:], h=outs[5], stream=handle)
+            for n in sizes:
+                torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want))
