@@ -123,7 +123,7 @@ inline size_t gated_workspace_up_to(int64_t N, int32_t d_in, int32_t F, int32_t 
 
 struct BackwardWorkspace {
     int32_t *offsets, *perm;
-    uint16_t *t2, *s2, *dh, *xt, *wt, *at, *bt;
+    uint16_t *t2, *s2, *dh, *xt, *at, *bt;
     float *planes;
     size_t outer_a;  // floats of planes that dA takes
     size_t bytes;
@@ -142,7 +142,6 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
     }
     w.dh = c.take<uint16_t>(size_t(padded_rows(N)) * 2 * F * 2);
     w.xt = c.take<uint16_t>(size_t(padded_rows(N)) * d_in * 2);
-    w.wt = c.take<uint16_t>(size_t(d_in) * 2 * F * 2);
     // fp32 sums of one product at a time: slices of K of t, s, dx and dW, pieces of the rows of dA and dB
     size_t floats = size_t(molora::gemm_plane_floats(N, d_in));
     floats = std::max(floats, size_t(molora::gemm_plane_floats(d_in, 2 * int64_t(F))));
@@ -327,7 +326,6 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
     int turns = 0;
     if (C > 0 && (dx || dA)) turn[turns++] = {Bb, w.bt, C, rank, 2 * F, rank};
     if (C > 0 && dx) turn[turns++] = {Ab, w.at, C, d_in, rank, d_in};
-    if (dx) turn[turns++] = {Wb, w.wt, 1, d_in, 2 * F, d_in};
     if (dW) turn[turns++] = {xb, w.xt, 1, N, d_in, Np};
     MOLORA_TRY(molora::launch_transposes(turn, turns, s));
     MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
@@ -346,11 +344,11 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
         MOLORA_TRY(molora::launch_grouped_outers(outer, outers, w.offsets, w.perm, N, C, rank, s));
     }
     if (dx)
-        MOLORA_TRY(molora::launch_gemm_bf16(w.dh, w.wt, w.at, w.s2, w.offsets, C > 0 ? w.perm : nullptr,
-                                            static_cast<uint16_t *>(dx), w.planes, N, 2 * F, d_in, C, rank, s));
+        MOLORA_TRY(molora::launch_gemm_bf16(w.dh, Wb, w.at, w.s2, w.offsets, C > 0 ? w.perm : nullptr,
+                                            static_cast<uint16_t *>(dx), w.planes, N, 2 * F, d_in, C, rank, true, s));
     if (dW)
         MOLORA_TRY(molora::launch_gemm_bf16(w.xt, w.dh, nullptr, nullptr, nullptr, nullptr, static_cast<uint16_t *>(dW), w.planes,
-                                            d_in, (int)Np, 2 * F, 0, 0, s));
+                                            d_in, (int)Np, 2 * F, 0, 0, false, s));
     return MOLORA_OK;
 }
 

@@ -192,17 +192,16 @@ inline int64_t gemm_plane_floats(int64_t N, int64_t d_out) {
 }
 hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                             const int32_t *offsets, const int32_t *perm, uint16_t *out, float *planes, int64_t N, int d_in,
-                            int d_out, int C, int rank, hipStream_t s);
+                            int d_out, int C, int rank, bool wt, hipStream_t s);
+// (wt: W is given as [d_out][d_in])
 struct GemmSlices {
     int slices, config;  // config -1: the streaming kernel
 };
-GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
+GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming);
 // h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr; planes as above
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                              const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, float *planes, int64_t N,
                              int d_in, int F, int C, int rank, int act, hipStream_t s);
-// the tile configuration that the cost rule takes where the streaming kernel is not to be had
-int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R);
 
 // ---- around the gated block (gated.hip) ----
 // at most 64 tokens (gated_decode.hip): h = base + the planes of the other slices + t B_r, z from it, h stored where
@@ -216,7 +215,7 @@ hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, 
 hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
                                 int act, hipStream_t s);
 // dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on; in one launch
-constexpr int kMaxTransposes = 4;
+constexpr int kMaxTransposes = 3;
 struct TransposeJob {
     const uint16_t *src;
     uint16_t *dst;

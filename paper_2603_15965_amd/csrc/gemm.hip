@@ -111,17 +111,15 @@ int gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming = t
 }
 }  // namespace
 
-int tiled_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) { return gemm_choice(N, d_in, d_out, C, R, false); }
-
 // The cheapest way to an output that is not h itself: one launch that ends in it, or fp32 sums in memory, of the
 // streaming kernel (many wide adapters against a small batch: its expand is the cheaper one) or of K in slices (few
 // output tiles, long K), and a second launch that ends them.
-GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R) {
+GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming) {
     GemmSlices pick{1, gemm_choice(N, d_in, d_out, C, R, false)};
     double best = tiled_cost(kGemmCosts[pick.config], N, d_in, d_out, C, R);
     const double floats = (double)N * d_out;
     const auto second = [&](int slices) { return 4.0 + slices * floats * 8 / 4e6; };  // (4 MB a microsecond, written and read)
-    if (N <= kSmallBatchMax && floats <= (double)kMaxPlaneFloats) {
+    if (streaming && N <= kSmallBatchMax && floats <= (double)kMaxPlaneFloats) {
         const double cost = streaming_cost(N, d_in, d_out, C, R) + second(1);
         if (cost < best) {
             best = cost;

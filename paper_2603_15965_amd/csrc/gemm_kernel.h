@@ -105,7 +105,9 @@ struct GemmEpilogue {
 
 // (two wavefronts per SIMD at least: with 512 registers to a wavefront the compiler keeps the accumulators in
 // the second half of them and moves some there and back in every tile)
-template <class Cfg, int OUT = kOutF32>
+// WT: W is given as [d_out][d_in], rows of k, the way a gradient meets the weight of its product: its tile lies in LDS as
+// the x tile does, and its fragments are read the same way.
+template <class Cfg, int OUT = kOutF32, bool WT = false>
 __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     const uint16_t *__restrict__ x, const uint16_t *__restrict__ W, const uint16_t *__restrict__ B,
     const uint16_t *__restrict__ t2, const int32_t *__restrict__ offsets,
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     if constexpr (OUT == kOutPlanes) {
         const int k0 = (int)blockIdx.y * ep.k_slice;
         x += k0;
-        W += (int64_t)k0 * d_out;
+        W += WT ? (int64_t)k0 : (int64_t)k0 * d_out;
         h += (int64_t)blockIdx.y * N * d_out;
         d_in = min(ep.k_slice, d_in - k0);
     }
@@ -205,6 +207,9 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         if (slot_is_a(i)) {
             row = piece_of(i) * Cfg::A_RPI + lane / Cfg::A_CPR;
             col = (lane % Cfg::A_CPR) ^ Cfg::swz_a(row);
+        } else if constexpr (WT) {  // column of the tile, 8-k chunk after the swizzle
+            row = (piece_of(i) - Cfg::A_PIECES) * Cfg::A_RPI + lane / Cfg::A_CPR;
+            col = (lane % Cfg::A_CPR) ^ Cfg::swz_a(row);
         } else {
             row = (piece_of(i) - Cfg::A_PIECES) * Cfg::B_RPI + lane / Cfg::B_CPR;
             const int pos = lane % Cfg::B_CPR;
@@ -219,12 +224,15 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     for (int i = 0; i < Cfg::LPW; ++i) {  // W pieces (the x pieces need the row table, below)
         int row, col;
         slot_geom(i, row, col);
-        off_g[i] = slot_is_a(i) ? 0u : (uint32_t)(((int64_t)row * d_out + col) * 2);
+        if constexpr (WT)
+            off_g[i] = slot_is_a(i) ? 0u : (uint32_t)(((int64_t)min(n0 + row, d_out - 1) * pitch + col * 8) * 2);
+        else
+            off_g[i] = slot_is_a(i) ? 0u : (uint32_t)(((int64_t)row * d_out + col) * 2);
     }
     // scalar bases of the full tiles, advanced per tile (x and W are < 4 GiB each)
     const unsigned char *a_base = (const unsigned char *)x;
     const unsigned char *b_base = (const unsigned char *)W;
-    const int64_t b_step = (int64_t)BK * d_out * 2;
+    const int64_t b_step = WT ? (int64_t)BK * 2 : (int64_t)BK * d_out * 2;
 
     auto issue_one = [&](unsigned char *stage, int i) __attribute__((always_inline)) {  // i-th load of a full tile
         load_to_lds16(slot_is_a(i) ? a_base : b_base, off_g[i], stage + piece_of(i) * 1024);
@@ -252,6 +260,9 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
                 const int k = T * BK + col * 8;
                 const int tok = tile_perm[row];
                 src = (k < d_in) ? x + (int64_t)(tok >= 0 ? tok : 0) * pitch + k : zero;
+            } else if constexpr (WT) {
+                const int k = T * BK + col * 8;
+                src = (k < d_in) ? W + (int64_t)min(n0 + row, d_out - 1) * pitch + k : zero;
             } else {
                 const int k = T * BK + row;
                 src = (k < d_in) ? W + (int64_t)k * d_out + col : zero;
@@ -425,15 +436,22 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     const uint32_t smem0 = (uint32_t)(uintptr_t)(MOLORA_LDS unsigned char *)smem;
     const int a_row = wm * (BM / Cfg::WM) + l16, b_row = kg * 8 + (l16 >> 2);
     const uint32_t pa_row = smem0 + a_row * Cfg::A_RB;
+    constexpr int NB = WT ? KS : TN;  // (WT: a fragment tn is an immediate offset of 16 rows, as of x)
     struct Addr {
-        uint32_t a[KS], b[TN];
+        uint32_t a[KS], b[NB];
     };
     Addr p0;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) p0.a[ks] = pa_row + (((4 * ks + kg) ^ Cfg::swz_a(a_row)) << 4);
+    if constexpr (WT) {
+        const int n_row = wn * (BN / Cfg::WN) + l16;
 #pragma unroll
-    for (int tn = 0; tn < TN; ++tn)
-        p0.b[tn] = smem0 + Cfg::A_BYTES + b_row * Cfg::B_RB + (Cfg::swz_b(wn * TN + tn, b_row) << 5) + (l16 & 3) * 8;
+        for (int ks = 0; ks < KS; ++ks) p0.b[ks] = smem0 + Cfg::A_BYTES + n_row * Cfg::A_RB + (((4 * ks + kg) ^ Cfg::swz_a(n_row)) << 4);
+    } else {
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn)
+            p0.b[tn] = smem0 + Cfg::A_BYTES + b_row * Cfg::B_RB + (Cfg::swz_b(wn * TN + tn, b_row) << 5) + (l16 & 3) * 8;
+    }
     // Addresses of the tile being multiplied (cur) and of the next one (nxt).  With two or three stages the hot
     // loop is unrolled by their number, so each copy knows its stage and reads through the constants in
     // `at`; elsewhere the stage offset is added once per tile.  (Three stages, formed per tile and unrolled: 655 x
@@ -445,14 +463,14 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) at[st].a[ks] = st == 0 ? p0.a[ks] : opaque(p0.a[ks] + st * Cfg::STAGE);
 #pragma unroll
-        for (int tn = 0; tn < TN; ++tn) at[st].b[tn] = st == 0 ? p0.b[tn] : opaque(p0.b[tn] + st * Cfg::STAGE);
+        for (int tn = 0; tn < NB; ++tn) at[st].b[tn] = st == 0 ? p0.b[tn] : opaque(p0.b[tn] + st * Cfg::STAGE);
     }
     auto stage_addresses = [&](Addr &ad, int T) {
         const uint32_t so = (uint32_t)(T % STAGES) * Cfg::STAGE;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) ad.a[ks] = opaque(p0.a[ks] + so);
 #pragma unroll
-        for (int tn = 0; tn < TN; ++tn) ad.b[tn] = opaque(p0.b[tn] + so);
+        for (int tn = 0; tn < NB; ++tn) ad.b[tn] = opaque(p0.b[tn] + so);
     };
     auto read_x = [](uint32_t p) __attribute__((always_inline)) -> bf16x8 {
         return *(const MOLORA_LDS bf16x8 *)(uintptr_t)p;
@@ -493,7 +511,10 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         fa[p % NA] = read_x(ad.a[p / TM] + (uint32_t)(p % TM) * (16 * Cfg::A_RB));
     };
     auto fetch_b = [&](const Addr &ad, int ks, int tn) __attribute__((always_inline)) {
-        fb[ks & 1][tn] = read_w(ad.b[tn] + (uint32_t)(ks * 32 * Cfg::B_RB));
+        if constexpr (WT)
+            fb[ks & 1][tn] = read_x(ad.b[ks] + (uint32_t)tn * (16 * Cfg::A_RB));
+        else
+            fb[ks & 1][tn] = read_w(ad.b[tn] + (uint32_t)(ks * 32 * Cfg::B_RB));
     };
     // loads return in order: tile T has landed once at most the loads of the `younger` tiles
     // issued after it are outstanding
@@ -638,7 +659,11 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         const uint32_t so_b = (uint32_t)(slab_area(e) - smem) - Cfg::A_BYTES - (kg >> 1) * (16 * Cfg::B_RB);  // (p0.b holds A_BYTES)
         uint32_t eb[TN];
 #pragma unroll
-        for (int tn = 0; tn < TN; ++tn) eb[tn] = p0.b[tn] + so_b;
+        for (int tn = 0; tn < TN; ++tn)
+            if constexpr (WT)
+                eb[tn] = smem0 + Cfg::A_BYTES + b_row * Cfg::B_RB + (Cfg::swz_b(wn * TN + tn, b_row) << 5) + (l16 & 3) * 8 + so_b;
+            else
+                eb[tn] = p0.b[tn] + so_b;
         const int sps = slabs_per_seg(q);
         if (grp != ((4 * b / sps) & ~63)) {
             grp = (4 * b / sps) & ~63;
@@ -774,9 +799,9 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
 }
 
 // more than 64 KB of dynamic LDS has to be asked for, once per device (see common.h)
-template <class Cfg, int OUT = kOutF32>
+template <class Cfg, int OUT = kOutF32, bool WT = false>
 struct GemmKernel {
-    static inline LdsRegistrar lds{(const void *)fused_gemm_kernel<Cfg, OUT>, Cfg::LDS_BYTES};
+    static inline LdsRegistrar lds{(const void *)fused_gemm_kernel<Cfg, OUT, WT>, Cfg::LDS_BYTES};
 };
 
 }  // namespace
