@@ -753,7 +753,7 @@ def molora_mx_quantize(x, codes=None, scales=None, stream=None):
         raise TypeError(f"x must be bfloat16 or float32, got {x.dtype}")
     codes, scales = _mx_outputs(rows, K, codes, scales, x)
     _call_here("molora_mx_quantize", _dev(x, x.dtype, "x"), int(x.dtype is torch.float32), *_mx(codes, scales, rows, K, "x"), rows, K,
-          _stream(stream))
+               _stream(stream))
     return codes, scales
 
 
@@ -808,8 +808,8 @@ def molora_apply_mx(x, wc, ws, A, B, r, h=None, workspace=None, stream=None):
     bf = torch.bfloat16
     work, work_bytes = _workspace("molora_apply_mx_workspace_bytes", (N, d_in, d_out, C, rank), workspace, x.device, stream)
     _call_here("molora_apply_mx", _dev(x, bf, "x"), *_mx(wc, ws, d_out, d_in, "W"), _dev(A, bf, "A", (C, d_in, rank)),
-          _dev(B, bf, "B", (C, rank, d_out)), _dev(r, torch.int32, "r", (N,)), _dev(h, torch.float32, "h", (N, d_out)),
-          N, d_in, d_out, C, rank, work, work_bytes, _stream(stream))
+               _dev(B, bf, "B", (C, rank, d_out)), _dev(r, torch.int32, "r", (N,)), _dev(h, torch.float32, "h", (N, d_out)),
+               N, d_in, d_out, C, rank, work, work_bytes, _stream(stream))
     return h
 
 
@@ -844,7 +844,7 @@ def molora_apply_gated(x, W, A=None, B=None, r=None, act="silu", z=None, pre=Non
         z = torch.empty((N, F), dtype=torch.bfloat16, device=x.device)
     work, work_bytes = _workspace("molora_apply_gated_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_apply_gated", *ops, _dev(z, torch.bfloat16, "z", (N, F)), _opt(pre, torch.float32, "pre", (N, 2 * F)), *sizes, code,
-          work, work_bytes, _stream(stream))
+               work, work_bytes, _stream(stream))
     return z
 
 
@@ -870,7 +870,7 @@ def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A
         out.append((t, _dev(t, bf, f"d{name}", shape)))
     work, work_bytes = _workspace("molora_gated_backward_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_gated_backward", _dev(dz, bf, "dz", (N, F)), *ops, _dev(pre, torch.float32, "pre", (N, 2 * F)), *(d for _, d in out),
-          *sizes, code, work, work_bytes, _stream(stream))
+               *sizes, code, work, work_bytes, _stream(stream))
     return tuple(t for t, _ in out)
 
 

@@ -268,8 +268,7 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
                                  void *workspace, size_t workspace_bytes, void *stream) {
     if (!gated_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
     if (N == 0) return MOLORA_OK;
-    if (!x || !W || !z || !adapters_given(A, B, r, C)) return MOLORA_EINVAL;
-    if (!workspace && carve_gated(nullptr, N, d_in, F, C, rank).bytes > 0) return MOLORA_EINVAL;
+    if (!x || !W || !z || !workspace || !adapters_given(A, B, r, C)) return MOLORA_EINVAL;
     if (!aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B) || !aligned16(r) || !aligned16(z) ||
         !aligned16(pre) || !aligned256(workspace))
         return MOLORA_EALIGN;
@@ -329,7 +328,7 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
     if (dW) turn[turns++] = {xb, w.xt, 1, N, d_in, Np};
     MOLORA_TRY(molora::launch_transposes(turn, turns, s));
     MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
-    if (C > 0) {
+    if (C > 0 && (dx || dA || dB)) {
         if (dB && N > kDecode)
             MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));
         else

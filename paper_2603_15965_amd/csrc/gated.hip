@@ -31,9 +31,9 @@ __global__ __launch_bounds__(256) void gate_kernel(const float *planes, int coun
     *(u32x2 *)(z + row * F + col) = bf16x4_bits(gate4(g, u, act));
 }
 
-// One thread takes four columns of a row.  dh is rounded to bf16 here: it is an operand of the matrix instructions in every gradient that follows.  (h comes
-// in fp32: with g and u rounded too, the gradients would be 1.9 instead of 1.4 times as far from their exact
-// values as their own rounding to bf16 puts them.)
+// One thread takes four columns of a row.  dh is rounded to bf16 here: it is an operand of the matrix instructions
+// in every gradient that follows.  (h comes in fp32: with g and u rounded too, the gradients would be 1.9 instead of
+// 1.4 times as far from their exact values as their own rounding to bf16 puts them.)
 __global__ __launch_bounds__(256) void gate_backward_kernel(const uint16_t *__restrict__ dz, const float *__restrict__ pre,
                                                             uint16_t *__restrict__ dh, int64_t N, int64_t items, int F, int act) {
     const int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4 *__restrict__ dst, int6
 // (rows of the padded side).  (t is padded to 66: a column is read without bank conflicts.)
 struct TransposeJobs {
     TransposeJob job[kMaxTransposes];
-    int first[kMaxTransposes + 1];  // its first workgroup
+    int first[kMaxTransposes];  // its first workgroup (past the last one: behind it)
 };
 __global__ __launch_bounds__(256) void transpose_kernel(TransposeJobs jobs) {
     __shared__ uint16_t t[64][66];
@@ -286,8 +286,6 @@ hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s) {
         blocks += jobs[i].batch * ((jobs[i].cols + 63) / 64) * ((jobs[i].padded + 63) / 64);
         if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
     }
-    all.first[kMaxTransposes] = (int)blocks;
-    for (int i = n; i < kMaxTransposes; ++i) all.first[i] = (int)blocks;
     hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)blocks), dim3(256), 0, s, all);
     return hipGetLastError();
 }

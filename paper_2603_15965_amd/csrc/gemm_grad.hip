@@ -9,9 +9,10 @@ hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t
     if (N == 0) return hipSuccess;
     // (the streaming kernel wants a dispatch, which dW has not, and W by rows of d_out)
     const GemmSlices pick = sliced_gemm_choice(N, d_in, d_out, C, rank, false);
+    const GemmEpilogue ep{out};
     if (pick.slices == 1)
-        return wt ? launch_config<kOutBf16, true>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, GemmEpilogue{out}, 1, s)
-                  : launch_config<kOutBf16, false>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, GemmEpilogue{out}, 1, s);
+        return wt ? launch_config<kOutBf16, true>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, ep, 1, s)
+                  : launch_config<kOutBf16, false>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, ep, 1, s);
     int count;
     const hipError_t e = wt ? launch_planes<true>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, count, s)
                             : launch_planes<false>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, count, s);

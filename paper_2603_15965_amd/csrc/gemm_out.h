@@ -16,7 +16,8 @@ hipError_t launch_out(const uint16_t *x, const uint16_t *W, const uint16_t *B, c
     const int tiles_n = (cols + per - 1) / per;
     const unsigned blocks = (unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8);
     constexpr auto kernel = fused_gemm_kernel<Cfg, OUT, WT>;
-    hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)slices), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
+    hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)slices), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h,
+                       (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
     return hipGetLastError();
 }
 
@@ -37,18 +38,17 @@ hipError_t launch_config(int config, const uint16_t *x, const uint16_t *W, const
 #undef MOLORA_OUT_ARGS
 }
 
-// fp32 sums of x W + t B_c to planes, `count` of them (the streaming kernel takes W by rows of d_out only)
+// fp32 sums of x W + t B_c over slices of K to planes, `count` of them
 template <bool WT>
 hipError_t launch_planes(const GemmSlices &pick, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                          const int32_t *offsets, const int32_t *perm, float *planes, int64_t N, int d_in, int d_out, int C,
                          int rank, int &count, hipStream_t s) {
-    count = 1;
-    if (pick.config < 0) return launch_small_batch_gemm(x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, Mix{1, C, nullptr, nullptr}, s);
     const int k_slice = ((d_in + pick.slices - 1) / pick.slices + 63) / 64 * 64;
     count = (d_in + k_slice - 1) / k_slice;
     return launch_config<kOutPlanes, WT>(pick.config, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank,
-                                     GemmEpilogue{nullptr, 0, k_slice}, count, s);
+                                         GemmEpilogue{nullptr, 0, k_slice}, count, s);
 }
+
 }  // namespace
 
 }  // namespace molora

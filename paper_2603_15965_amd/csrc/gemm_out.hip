@@ -10,9 +10,13 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
     if (N == 0) return hipSuccess;
     const GemmSlices pick = sliced_gemm_choice(N, d_in, 2 * F, C, rank, perm != nullptr);
     if (pick.slices == 1 && pick.config >= 0)
-        return launch_config<kOutGated, false>(pick.config, x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C, rank, GemmEpilogue{z, act}, 1, s);
-    int count;
-    const hipError_t e = launch_planes<false>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, count, s);
+        return launch_config<kOutGated, false>(pick.config, x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C, rank,
+                                               GemmEpilogue{z, act}, 1, s);
+    int count = 1;
+    const hipError_t e =
+        pick.config < 0
+            ? launch_small_batch_gemm(x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, Mix{1, C, nullptr, nullptr}, s)
+            : launch_planes<false>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, count, s);
     return e != hipSuccess ? e : launch_gate(planes, count, z, pre, N, F, act, s);
 }
 
