@@ -145,9 +145,9 @@ inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int
     // fp32 sums of one product at a time: slices of K of t, s, dx and dW, pieces of the rows of dA and dB
     size_t floats = size_t(molora::gemm_plane_floats(N, d_in));
     floats = std::max(floats, size_t(molora::gemm_plane_floats(d_in, 2 * int64_t(F))));
-    w.outer_a = C > 0 ? round256(molora::grouped_outer_floats(N, d_in, C, rank) * 4) / 4 : 0;
+    w.outer_a = C > 0 ? round256(molora::grouped_outer_floats(N, d_in, rank) * 4) / 4 : 0;
     if (C > 0) {
-        floats = std::max(floats, w.outer_a + molora::grouped_outer_floats(N, 2 * F, C, rank));
+        floats = std::max(floats, w.outer_a + molora::grouped_outer_floats(N, 2 * F, rank));
         floats = std::max(floats, std::max(shrink_scratch_up_to(N, d_in, C, rank), shrink_scratch_up_to(N, 2 * F, C, rank)) / 4);
     }
     w.planes = c.take<float>(floats * 4);

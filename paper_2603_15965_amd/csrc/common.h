@@ -232,7 +232,7 @@ struct GroupedOuter {
     int D;
     bool flat;
 };
-size_t grouped_outer_floats(int64_t N, int D, int C, int R);
+size_t grouped_outer_floats(int64_t N, int D, int R);
 hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t *offsets, const int32_t *perm, int64_t N, int C,
                                  int R, hipStream_t s);
 // out [n] bf16 = the sum of `count` planes of n floats (a multiple of 8)

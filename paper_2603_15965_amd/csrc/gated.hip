@@ -1,6 +1,8 @@
 // The backward pass of the gated block z = act(g) u, [g | u] = h = x W + (x A_r) B_r, beside its GEMMs:
 //
 //     dh = [dz u act'(g) | dz act(g)],   dA_c = x_c^T (dh_c B_c^T),   dB_c = (x_c A_c)^T dh_c
+#include <algorithm>
+
 #include "gate.h"
 #include "lds_dma.h"
 
@@ -106,19 +108,51 @@ __global__ __launch_bounds__(256) void transpose_kernel(TransposeJobs jobs) {
 // out_c = Y_c^T S_c over the rows of a bucket.  A workgroup takes 64 columns of Y and 32 of S (the hi and the lo
 // half of each); its four wavefronts take 32 rows at a time in turn, the next ones on their way while these are
 // multiplied, bring them to LDS as they lie in memory and read both operands through the transpose read (k of the product
-// runs down the rows).  Sums are added in wavefront order.  Where the columns leave the chip idle, the rows of a bucket
-// are cut into `cuts` pieces of their own workgroups: fp32 sums to planes, added by a second launch in a fixed order.
-constexpr int kOuterCols = 64, kOuterR = 32;
+// runs down the rows).  Sums are added in wavefront order.
+// A bucket of more than `rows` rows is cut into even pieces of their own workgroups, whose fp32 sums go to planes and are
+// added by a second launch in a fixed order.  The launch has a piece for every bucket and then as many more as there
+// can be (N / rows), whichever buckets turn out to be the long ones; `rows` is what the workgroups of a compute unit
+// share evenly.  It is bound by reading dh and x: 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16, level routing, 48 us
+// (235 MB).  16384 x 512 -> 2 x 1024, 48 of rank 128 and one of them for all tokens: 84 us, in whole buckets 129; with
+// level routing cut buckets cost the second launch, 5 us.
+constexpr int kOuterCols = 64, kOuterR = 32, kOuterRows = 1024;
 struct OuterJob {
     const uint16_t *y, *s2;
     uint16_t *out;
-    float *planes;  // [cuts][C][D][R] (flat: [R][D]) where cuts > 1
-    int D, flat, cuts, tiles;  // tiles: column tiles of Y
+    float *planes;  // [2 extra][D][R] (flat: [R][D]): the further pieces, then the first ones of the same buckets
+    int D, flat, tiles, rows, extra;  // tiles: column tiles of Y
 };
 struct OuterJobs {
     OuterJob job[2];
-    int first;  // the second one's first workgroup
+    int first, first_sum;  // the second one's first workgroup, of the products and of the sums
 };
+// A piece of a bucket: its cut-th of n; `first`: the place of the bucket's second piece among all further ones.
+struct Piece {
+    int c, cut, n, first;
+};
+// The further piece j of all, or (j < 0) the first one of bucket c; c = -1: there are fewer.
+__device__ __forceinline__ Piece find_piece(const int32_t *__restrict__ offsets, int C, int rows, int j, int c, int lane) {
+    int before = 0;
+    for (int c0 = 0; c0 < C; c0 += 64) {
+        const int at = min(c0 + lane, C - 1), len = offsets[at + 1] - offsets[at];
+        const int more = c0 + lane < C && len > 0 ? (len - 1) / rows : 0;
+        int sum = more;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(sum, d);
+            if (lane >= d) sum += up;
+        }
+        sum += before;
+        const uint64_t here = __ballot(j < 0 ? c0 + lane == c : sum > j);
+        if (here != 0) {
+            const int l = __builtin_ctzll(here);
+            const int n = __builtin_amdgcn_readlane(more, l) + 1, first = __builtin_amdgcn_readlane(sum, l) - n + 1;
+            return Piece{c0 + l, j < 0 ? 0 : j - first + 1, n, first};
+        }
+        before = __builtin_amdgcn_readlane(sum, 63);
+    }
+    return Piece{-1, 0, 0, 0};
+}
 __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block, const int32_t *__restrict__ offsets,
                                                    const int32_t *__restrict__ perm, int C, int R, unsigned char *lds) {
     constexpr int YS = kOuterCols * 2 + 32, SS = kOuterR * 4 + 32;  // bytes per row in LDS
@@ -128,11 +162,18 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
     const int kq = lane >> 4, l16 = lane & 15;
     const int D = m.D, parts = (R + kOuterR - 1) / kOuterR;
     const int d0 = block % m.tiles * kOuterCols, r0 = block / m.tiles % parts * kOuterR;
-    const int cut = block / (m.tiles * parts) % m.cuts, c = block / (m.tiles * parts * m.cuts);
+    const int p_at = block / (m.tiles * parts);
+    Piece piece{p_at, 0, 1, 0};
+    if (p_at >= C)
+        piece = find_piece(offsets, C, m.rows, p_at - C, -1, lane);
+    else if (offsets[p_at + 1] - offsets[p_at] > m.rows)
+        piece = find_piece(offsets, C, m.rows, -1, p_at, lane);
+    const int c = piece.c;
+    if (c < 0) return;
     int lo = offsets[c], hi = offsets[c + 1];
-    if (m.cuts > 1) {  // pieces of whole steps
-        const int per = ((hi - lo + m.cuts - 1) / m.cuts + 127) & ~127;
-        lo = min(lo + cut * per, hi);
+    if (piece.n > 1) {  // pieces of whole steps
+        const int per = ((hi - lo + piece.n - 1) / piece.n + 127) & ~127;
+        lo = min(lo + piece.cut * per, hi);
         hi = min(lo + per, hi);
     }
     unsigned char *ys = lds + wave * SLAB, *ss = ys + 32 * YS;
@@ -200,11 +241,11 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
             for (int k = 0; k < 2; ++k)
                 v[k] += ((const float *)(lds + w * PART))[(d + (m.flat ? k : 0)) * (kOuterR + 1) + r + (m.flat ? 0 : k)];
         if (d0 + d < D && r0 + r < R) {
-            const int64_t at = m.flat ? ((int64_t)c * R + r0 + r) * D + d0 + d : ((int64_t)c * D + d0 + d) * R + r0 + r;
-            if (m.cuts > 1)
-                *(f32x2_t *)(m.planes + (int64_t)cut * C * D * R + at) = f32x2_t{v[0], v[1]};
+            const int64_t at = m.flat ? (int64_t)(r0 + r) * D + d0 + d : (int64_t)(d0 + d) * R + r0 + r, all = (int64_t)D * R;
+            if (piece.n > 1)
+                *(f32x2_t *)(m.planes + (piece.cut > 0 ? piece.first + piece.cut - 1 : m.extra + piece.first) * all + at) = f32x2_t{v[0], v[1]};
             else
-                *(uint32_t *)(m.out + at) = bf16x2_bits(v[0], v[1]);
+                *(uint32_t *)(m.out + c * all + at) = bf16x2_bits(v[0], v[1]);
         }
     }
 }
@@ -216,37 +257,46 @@ __global__ __launch_bounds__(256) void grouped_outer_kernel(OuterJobs jobs, cons
     grouped_outer_body(jobs.job[second ? 1 : 0], (int)blockIdx.x - (second ? jobs.first : 0), offsets, perm, C, R, lds);
 }
 
-// bf16 sums of fp32 planes, eight values to a thread; two arrays in one launch.
-struct SumJob {
-    const float *planes;
-    uint16_t *out;
-    int64_t n;  // values, a multiple of 8
-    int planes_n;
-};
-struct SumJobs {
-    SumJob job[2];
-    int first;
-};
-__global__ __launch_bounds__(256) void sum_planes_kernel(SumJobs jobs) {
-    const bool second = (int)blockIdx.x >= jobs.first;
-    const SumJob &m = jobs.job[second ? 1 : 0];
-    const int64_t at = ((int64_t)((int)blockIdx.x - (second ? jobs.first : 0)) * 256 + threadIdx.x) * 8;
-    if (at >= m.n) return;
-    f32x4 a = *(const f32x4 *)(m.planes + at), b = *(const f32x4 *)(m.planes + at + 4);
-    for (int i = 1; i < m.planes_n; ++i) {
-        a += *(const f32x4 *)(m.planes + i * m.n + at);
-        b += *(const f32x4 *)(m.planes + i * m.n + at + 4);
+// bf16 sums of fp32 planes, eight values to a thread.
+__global__ __launch_bounds__(256) void sum_planes_kernel(const float *__restrict__ planes, uint16_t *__restrict__ out, int64_t n,
+                                                         int count) {
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= n) return;
+    f32x4 a = *(const f32x4 *)(planes + at), b = *(const f32x4 *)(planes + at + 4);
+    for (int i = 1; i < count; ++i) {
+        a += *(const f32x4 *)(planes + i * n + at);
+        b += *(const f32x4 *)(planes + i * n + at + 4);
     }
     const u32x2 lo = bf16x4_bits(a), hi = bf16x4_bits(b);
-    *(u32x4 *)(m.out + at) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    *(u32x4 *)(out + at) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+// The same of the pieces of the buckets that were cut: 2048 values to the workgroup of a bucket's second piece.
+__global__ __launch_bounds__(256) void sum_pieces_kernel(OuterJobs jobs, const int32_t *__restrict__ offsets, int C, int R) {
+    const bool second = (int)blockIdx.x >= jobs.first_sum;
+    const OuterJob &m = jobs.job[second ? 1 : 0];
+    const int block = (int)blockIdx.x - (second ? jobs.first_sum : 0);
+    const int64_t n = (int64_t)m.D * R;
+    const int chunks = (int)((n + 2047) / 2048);
+    const Piece piece = find_piece(offsets, C, m.rows, block / chunks, -1, threadIdx.x & 63);
+    const int64_t at = ((int64_t)(block % chunks) * 256 + threadIdx.x) * 8;
+    if (piece.c < 0 || piece.cut != 1 || at >= n) return;
+    const float *p = m.planes + (m.extra + piece.first) * n + at;
+    f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+    p = m.planes + piece.first * n + at;
+    for (int i = 1; i < piece.n; ++i, p += n) {
+        a += *(const f32x4 *)p;
+        b += *(const f32x4 *)(p + 4);
+    }
+    const u32x2 lo = bf16x4_bits(a), hi = bf16x4_bits(b);
+    *(u32x4 *)(m.out + piece.c * n + at) = u32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-int outer_cuts(int64_t N, int D, int C, int R) {
-    const int64_t blocks = (int64_t)((D + kOuterCols - 1) / kOuterCols) * ((R + kOuterR - 1) / kOuterR) * C;
-    // enough workgroups for two to a compute unit, and four steps of 128 rows to a piece of an average bucket
-    int64_t cuts = 512 / blocks, most = N / ((int64_t)C * 512);
-    if (cuts > most) cuts = most;
-    return (int)(cuts < 1 ? 1 : cuts > 16 ? 16 : cuts);
+// workgroups of a piece
+int64_t outer_tiles(int D, int R) { return (int64_t)((D + kOuterCols - 1) / kOuterCols) * ((R + kOuterR - 1) / kOuterR); }
+// rows of a piece: so many that two workgroups to a compute unit share all rows, and eight steps at least
+int outer_rows(int64_t N, int D, int R) {
+    const int64_t rows = (N * outer_tiles(D, R) + 511) / 512;
+    return (int)(rows <= kOuterRows ? kOuterRows : (rows + 127) / 128 * 128);
 }
 
 }  // namespace
@@ -290,18 +340,14 @@ hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s) {
     return hipGetLastError();
 }
 
-size_t grouped_outer_floats(int64_t N, int D, int C, int R) {
-    const int cuts = outer_cuts(N, D, C, R);
-    return cuts > 1 ? (size_t)cuts * C * D * R : 0;
+size_t grouped_outer_floats(int64_t N, int D, int R) {  // (never less for more rows: what outer_rows gives at most)
+    return (size_t)(std::min(N / kOuterRows, 512 / outer_tiles(D, R)) * 2) * D * R;
 }
 
 hipError_t launch_sum_planes(const float *planes, uint16_t *out, int64_t n, int count, hipStream_t s) {
     const int64_t blocks = (n + 2047) / 2048;
     if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
-    SumJobs jobs{};
-    jobs.job[0] = SumJob{planes, out, n, count};
-    jobs.first = (int)blocks;
-    hipLaunchKernelGGL(sum_planes_kernel, dim3((unsigned)blocks), dim3(256), 0, s, jobs);
+    hipLaunchKernelGGL(sum_planes_kernel, dim3((unsigned)blocks), dim3(256), 0, s, planes, out, n, count);
     return hipGetLastError();
 }
 
@@ -309,28 +355,21 @@ hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t 
                                  int R, hipStream_t s) {
     if (n < 1 || n > 2) return n == 0 ? hipSuccess : hipErrorInvalidValue;
     OuterJobs jobs{};
-    SumJobs sums{};
-    int64_t blocks = 0, sum_blocks = 0;
-    int n_sums = 0;
+    int64_t blocks = 0, sums = 0;
     for (int i = 0; i < n; ++i) {
         OuterJob &m = jobs.job[i];
-        m = OuterJob{want[i].y, want[i].s2, want[i].out, want[i].planes, want[i].D, want[i].flat ? 1 : 0, outer_cuts(N, want[i].D, C, R),
-                     (want[i].D + kOuterCols - 1) / kOuterCols};
-        if (i == 1) jobs.first = (int)blocks;
-        blocks += (int64_t)m.tiles * ((R + kOuterR - 1) / kOuterR) * m.cuts * C;
-        if (m.cuts > 1) {
-            if (n_sums == 1) sums.first = (int)sum_blocks;
-            sums.job[n_sums++] = SumJob{m.planes, m.out, (int64_t)C * m.D * R, m.cuts};
-            sum_blocks += ((int64_t)C * m.D * R + 2047) / 2048;
-        }
+        const int rows = outer_rows(N, want[i].D, R), extra = (int)(N / rows);
+        m = OuterJob{want[i].y, want[i].s2, want[i].out, want[i].planes, want[i].D, want[i].flat ? 1 : 0,
+                     (want[i].D + kOuterCols - 1) / kOuterCols, rows, extra};
+        blocks += outer_tiles(m.D, R) * (C + extra);
+        sums += ((int64_t)m.D * R + 2047) / 2048 * extra;
+        if (i == 0) jobs.first = (int)blocks, jobs.first_sum = (int)sums;
+        if (blocks >= (int64_t(1) << 24) || sums >= (int64_t(1) << 24)) return hipErrorInvalidValue;
     }
-    if (n == 1) jobs.first = (int)blocks;
-    if (blocks >= (int64_t(1) << 24) || sum_blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
     hipLaunchKernelGGL(grouped_outer_kernel, dim3((unsigned)blocks), dim3(256), 0, s, jobs, offsets, perm, C, R);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || n_sums == 0) return e;
-    if (n_sums == 1) sums.first = (int)sum_blocks;
-    hipLaunchKernelGGL(sum_planes_kernel, dim3((unsigned)sum_blocks), dim3(256), 0, s, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sums == 0) return e;
+    hipLaunchKernelGGL(sum_pieces_kernel, dim3((unsigned)sums), dim3(256), 0, s, jobs, offsets, C, R);
     return hipGetLastError();
 }
 

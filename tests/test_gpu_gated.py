@@ -26,6 +26,8 @@ def _case(N, d_in, F, C, rank, how="mixed", seed=0):
         r[:] = -1
     elif how == "last":
         r[:] = C - 1
+    elif how == "ends":   # two long buckets, short and empty ones between them
+        r[:N * 3 // 10], r[N * 4 // 10:] = 0, C - 1
     dz = wl.to_bf16_bits(rng.standard_normal((N, F)).astype(np.float32))
     return w, r, dz
 
@@ -74,7 +76,8 @@ BACKWARD = [(1, 64, 8, 1, 8, "last"), (1, 64, 8, 2, 8, "none"), (7, 136, 40, 3, 
             (65, 72, 24, 2, 128, "mixed"), (130, 264, 200, 5, 40, "mixed"), (515, 520, 264, 7, 24, "mixed"), (300, 128, 136, 40, 16, "mixed"),
             (33, 136, 72, 0, 0, "none"), (200, 264, 136, 0, 0, "none"), (257, 64, 64, 3, 8, "none"),
             # few output tiles: K in slices (of dx: 2 F, of dW: the tokens), rows of a bucket in pieces, the last ones ragged
-            (96, 72, 1040, 2, 16, "mixed"), (2056, 64, 40, 2, 16, "mixed"), (3001, 136, 72, 1, 40, "last"), (1500, 64, 1032, 0, 0, "none")]
+            (96, 72, 1040, 2, 16, "mixed"), (2056, 64, 40, 2, 16, "mixed"), (3001, 136, 72, 1, 40, "last"), (1500, 64, 1032, 0, 0, "none"),
+            (4100, 72, 40, 70, 24, "last"), (5003, 64, 72, 131, 8, "ends")]
 
 
 @pytest.mark.parametrize("N,d_in,F,C,rank,how,act", [c + (ACTS[i % 3],) for i, c in enumerate(BACKWARD)])
