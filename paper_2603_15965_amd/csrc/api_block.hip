@@ -326,8 +326,7 @@ molora_status molora_gated_backward(const void *dz, const void *x, const void *W
     if (C > 0 && (dx || dA)) turn[turns++] = {Bb, w.bt, C, rank, 2 * F, rank};
     if (C > 0 && dx) turn[turns++] = {Ab, w.at, C, d_in, rank, d_in};
     if (dW) turn[turns++] = {xb, w.xt, 1, N, d_in, Np};
-    MOLORA_TRY(molora::launch_transposes(turn, turns, s));
-    MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, s));
+    MOLORA_TRY(molora::launch_gate_backward(static_cast<const uint16_t *>(dz), pre, w.dh, N, Np, F, act, turn, turns, s));
     if (C > 0 && (dx || dA || dB)) {
         if (dB && N > kDecode)
             MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));

@@ -211,17 +211,16 @@ hipError_t launch_gated_finish(const float *base, const float *planes, int slice
                                int act, hipStream_t s);
 // h = the sum of `count` planes [N][2 F], z from it, h stored where pre != nullptr
 hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, int64_t N, int F, int act, hipStream_t s);
-// dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F]; rows N .. padded - 1 are zero
-hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
-                                int act, hipStream_t s);
-// dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on; in one launch
+// dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F], rows N .. padded - 1 zero; in the same launch, for n jobs,
+// dst [batch][cols][padded] = src [batch][rows][cols] transposed, zero from row `rows` on
 constexpr int kMaxTransposes = 3;
 struct TransposeJob {
     const uint16_t *src;
     uint16_t *dst;
     int64_t batch, rows, cols, padded;
 };
-hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s);
+hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
+                                int act, const TransposeJob *jobs, int n, hipStream_t s);
 // out[c] = sum over the positions p of bucket c of outer(y[perm[p]], s_p), bf16: [D][R], or [R][D] when flat;
 // y [N][D], s2 [N][2 R] in the layout of the shrink's output.  Empty buckets give zeros.  planes: scratch of
 // grouped_outer_floats(...) floats.

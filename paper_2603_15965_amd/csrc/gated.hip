@@ -36,28 +36,35 @@ __global__ __launch_bounds__(256) void gate_kernel(const float *planes, int coun
 // One thread takes four columns of a row.  dh is rounded to bf16 here: it is an operand of the matrix instructions
 // in every gradient that follows.  (h comes in fp32: with g and u rounded too, the gradients would be 1.9 instead of
 // 1.4 times as far from their exact values as their own rounding to bf16 puts them.)
-__global__ __launch_bounds__(256) void gate_backward_kernel(const uint16_t *__restrict__ dz, const float *__restrict__ pre,
-                                                            uint16_t *__restrict__ dh, int64_t N, int64_t items, int F, int act) {
-    const int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (it >= items) return;
+struct GateBackward {
+    const uint16_t *dz;
+    const float *pre;
+    uint16_t *dh;
+    int64_t N, items;
+    int F, act;
+};
+__device__ __forceinline__ void gate_backward_body(const GateBackward &m, int64_t block) {
+    const int64_t it = block * 256 + threadIdx.x;
+    if (it >= m.items) return;
+    const int F = m.F;
     const int per = F / 4;
     const int64_t row = it / per;
     const int col = (int)(it % per) * 4;
-    uint16_t *out = dh + row * 2 * F + col;
-    if (row >= N) {
+    uint16_t *out = m.dh + row * 2 * F + col;
+    if (row >= m.N) {
         *(u32x2 *)out = u32x2{0, 0};
         *(u32x2 *)(out + F) = u32x2{0, 0};
         return;
     }
-    const float *h = pre + row * 2 * F + col;
+    const float *h = m.pre + row * 2 * F + col;
     const f32x4 g = *(const f32x4 *)h, u = *(const f32x4 *)(h + F);
-    const u32x2 d2 = *(const u32x2 *)(dz + row * F + col);
+    const u32x2 d2 = *(const u32x2 *)(m.dz + row * F + col);
     f32x4 dg, du;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float d = bf16_bits_to_f32((d2[i >> 1] >> (16 * (i & 1))) & 0xFFFF);
         float slope;
-        const float p = gate_factor<true>(g[i], act, slope);
+        const float p = gate_factor<true>(g[i], m.act, slope);
         dg[i] = d * u[i] * (p + g[i] * slope);
         du[i] = d * g[i] * p;
     }
@@ -69,14 +76,19 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4 *__restrict__ dst, int6
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) dst[i] = u32x4{0, 0, 0, 0};
 }
 
-// Several matrices transposed in one launch, 64 x 64 elements at a time through LDS.  Rows and columns are multiples of 8
-// (rows of the padded side).  (t is padded to 66: a column is read without bank conflicts.)
+// The first launch of a backward pass: dh, and matrices transposed, 64 x 64 elements at a time through LDS (a step of
+// 515 tokens takes 4 us less than with two launches).  Rows and columns are multiples of 8 (rows of the padded side).
+// (t is padded to 66: a column is read without bank conflicts.)
 struct TransposeJobs {
     TransposeJob job[kMaxTransposes];
-    int first[kMaxTransposes];  // its first workgroup (past the last one: behind it)
+    int first[kMaxTransposes + 1];  // its first workgroup (past the last one: behind it); behind all: the gate's
 };
-__global__ __launch_bounds__(256) void transpose_kernel(TransposeJobs jobs) {
+__global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward gate, TransposeJobs jobs) {
     __shared__ uint16_t t[64][66];
+    if ((int)blockIdx.x >= jobs.first[kMaxTransposes]) {
+        gate_backward_body(gate, (int)blockIdx.x - jobs.first[kMaxTransposes]);
+        return;
+    }
     int j = 0;
 #pragma unroll
     for (int i = 1; i < kMaxTransposes; ++i) j += (int)blockIdx.x >= jobs.first[i] ? 1 : 0;
@@ -316,16 +328,7 @@ hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, 
 }
 
 hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *dh, int64_t N, int64_t padded, int F,
-                                int act, hipStream_t s) {
-    const int64_t items = padded * (F / 4), blocks = (items + 255) / 256;
-    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
-    if (blocks > 0)
-        hipLaunchKernelGGL(gate_backward_kernel, dim3((unsigned)blocks), dim3(256), 0, s, dz, pre, dh, N, items, F, act);
-    return hipGetLastError();
-}
-
-hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s) {
-    if (n == 0) return hipSuccess;
+                                int act, const TransposeJob *jobs, int n, hipStream_t s) {
     if (n > kMaxTransposes) return hipErrorInvalidValue;
     TransposeJobs all{};
     int64_t blocks = 0;
@@ -336,7 +339,11 @@ hipError_t launch_transposes(const TransposeJob *jobs, int n, hipStream_t s) {
         blocks += jobs[i].batch * ((jobs[i].cols + 63) / 64) * ((jobs[i].padded + 63) / 64);
         if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
     }
-    hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)blocks), dim3(256), 0, s, all);
+    all.first[kMaxTransposes] = (int)blocks;
+    const GateBackward gate{dz, pre, dh, N, padded * (F / 4), F, act};
+    blocks += (gate.items + 255) / 256;
+    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(gate_backward_kernel, dim3((unsigned)blocks), dim3(256), 0, s, gate, all);
     return hipGetLastError();
 }
 
