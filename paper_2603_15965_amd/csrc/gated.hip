@@ -127,12 +127,16 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward gate, T
 // share evenly.  It is bound by reading dh and x: 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16, level routing, 48 us
 // (235 MB).  16384 x 512 -> 2 x 1024, 48 of rank 128 and one of them for all tokens: 84 us, in whole buckets 129; with
 // level routing cut buckets cost the second launch, 5 us.
-constexpr int kOuterCols = 64, kOuterR = 32, kOuterRows = 1024;
+// Where the buckets are short on average (kWideRows) and the columns many, the wavefronts take 64 columns of Y each instead,
+// all rows and no sum: with one step of rows to a bucket three of four had nothing to do.  168 x 1792 -> 2 x 1536, 59 of
+// rank 40: 33 -> 20 us; 8192 x 2048 -> 2 x 6144, 64 of rank 16: 72 -> 56; at 4096 rows and 64 skewed ones of rank 32 31 -> 35;
+// up to 512 rows to a bucket nothing is gained.
+constexpr int kOuterCols = 64, kOuterR = 32, kOuterRows = 1024, kWideRows = 128;
 struct OuterJob {
     const uint16_t *y, *s2;
     uint16_t *out;
     float *planes;  // [2 extra][D][R] (flat: [R][D]): the further pieces, then the first ones of the same buckets
-    int D, flat, tiles, rows, extra;  // tiles: column tiles of Y
+    int D, flat, tiles, rows, extra, wide;  // tiles: column tiles of Y
 };
 struct OuterJobs {
     OuterJob job[2];
@@ -173,7 +177,7 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int kq = lane >> 4, l16 = lane & 15;
     const int D = m.D, parts = (R + kOuterR - 1) / kOuterR;
-    const int d0 = block % m.tiles * kOuterCols, r0 = block / m.tiles % parts * kOuterR;
+    const int d0 = (block % m.tiles * (m.wide ? 4 : 1) + (m.wide ? wave : 0)) * kOuterCols, r0 = block / m.tiles % parts * kOuterR;
     const int p_at = block / (m.tiles * parts);
     Piece piece{p_at, 0, 1, 0};
     if (p_at >= C)
@@ -210,9 +214,10 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
             sv[i] = *(const u32x4 *)(s_col + (int64_t)p * 2 * R);
         }
     };
-    int p0 = lo + wave * 32;
+    int p0 = m.wide ? lo : lo + wave * 32;
+    const int step = m.wide ? 32 : 128;
     if (p0 < hi) load(p0);
-    for (; p0 < hi; p0 += 128) {
+    for (; p0 < hi; p0 += step) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (p0 + i * 8 + row >= hi) {  // rows of the next bucket count as zero, on both sides
@@ -222,7 +227,7 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
             *(u32x4 *)(ys + (i * 8 + row) * YS + col * 2) = yv[i];
             *(u32x4 *)(ss + (i * 8 + row) * SS + col * 2) = sv[i];
         }
-        if (p0 + 128 < hi) load(p0 + 128);
+        if (p0 + step < hi) load(p0 + step);
         bf16x8 fy[4], fs[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -244,20 +249,28 @@ __device__ __forceinline__ void grouped_outer_body(const OuterJob &m, int block,
 #pragma unroll
             for (int v = 0; v < 4; ++v) part[(i * 16 + kq * 4 + v) * (kOuterR + 1) + j * 16 + l16] = acc[i][j][v];
     __syncthreads();
-    for (int it = tid; it < kOuterCols * kOuterR / 2; it += 256) {  // two neighbours of the output's rows
-        const int d = m.flat ? it % (kOuterCols / 2) * 2 : it / (kOuterR / 2), r = m.flat ? it / (kOuterCols / 2) : it % (kOuterR / 2) * 2;
-        float v[2] = {0.f, 0.f};
+    constexpr int ITEMS = kOuterCols * kOuterR / 2;  // two neighbours of the output's rows each
+    const int first_d = d0 - (m.wide ? wave * kOuterCols : 0);
+    for (int at = tid; at < (m.wide ? 4 * ITEMS : ITEMS); at += 256) {
+        const int it = at % ITEMS, from = at / ITEMS;
+        int d = m.flat ? it % (kOuterCols / 2) * 2 : it / (kOuterR / 2), r = m.flat ? it / (kOuterCols / 2) : it % (kOuterR / 2) * 2;
+        const int place = d * (kOuterR + 1) + r, next = m.flat ? kOuterR + 1 : 1;
+        const float *const p = (const float *)(lds + from * PART) + place;
+        float v[2] = {p[0], p[next]};
+        if (!m.wide) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                v[k] += ((const float *)(lds + w * PART))[(d + (m.flat ? k : 0)) * (kOuterR + 1) + r + (m.flat ? 0 : k)];
-        if (d0 + d < D && r0 + r < R) {
-            const int64_t at = m.flat ? (int64_t)(r0 + r) * D + d0 + d : (int64_t)(d0 + d) * R + r0 + r, all = (int64_t)D * R;
+            for (int w = 1; w < 4; ++w) {
+                v[0] += ((const float *)(lds + w * PART))[place];
+                v[1] += ((const float *)(lds + w * PART))[place + next];
+            }
+        }
+        d += first_d + from * kOuterCols;
+        if (d < D && r0 + r < R) {
+            const int64_t to = m.flat ? (int64_t)(r0 + r) * D + d : (int64_t)d * R + r0 + r, all = (int64_t)D * R;
             if (piece.n > 1)
-                *(f32x2_t *)(m.planes + (piece.cut > 0 ? piece.first + piece.cut - 1 : m.extra + piece.first) * all + at) = f32x2_t{v[0], v[1]};
+                *(f32x2_t *)(m.planes + (piece.cut > 0 ? piece.first + piece.cut - 1 : m.extra + piece.first) * all + to) = f32x2_t{v[0], v[1]};
             else
-                *(uint32_t *)(m.out + c * all + at) = bf16x2_bits(v[0], v[1]);
+                *(uint32_t *)(m.out + c * all + to) = bf16x2_bits(v[0], v[1]);
         }
     }
 }
@@ -366,9 +379,11 @@ hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t 
     for (int i = 0; i < n; ++i) {
         OuterJob &m = jobs.job[i];
         const int rows = outer_rows(N, want[i].D, R), extra = (int)(N / rows);
+        const int tiles = (want[i].D + kOuterCols - 1) / kOuterCols, parts = (R + kOuterR - 1) / kOuterR;
+        const bool wide = N <= (int64_t)C * kWideRows && (int64_t)tiles * parts * C > 1024;
         m = OuterJob{want[i].y, want[i].s2, want[i].out, want[i].planes, want[i].D, want[i].flat ? 1 : 0,
-                     (want[i].D + kOuterCols - 1) / kOuterCols, rows, extra};
-        blocks += outer_tiles(m.D, R) * (C + extra);
+                     wide ? (tiles + 3) / 4 : tiles, rows, extra, wide ? 1 : 0};
+        blocks += (int64_t)m.tiles * parts * (C + extra);
         sums += ((int64_t)m.D * R + 2047) / 2048 * extra;
         if (i == 0) jobs.first = (int)blocks, jobs.first_sum = (int)sums;
         if (blocks >= (int64_t(1) << 24) || sums >= (int64_t(1) << 24)) return hipErrorInvalidValue;

@@ -77,7 +77,8 @@ BACKWARD = [(1, 64, 8, 1, 8, "last"), (1, 64, 8, 2, 8, "none"), (7, 136, 40, 3, 
             (33, 136, 72, 0, 0, "none"), (200, 264, 136, 0, 0, "none"), (257, 64, 64, 3, 8, "none"),
             # few output tiles: K in slices (of dx: 2 F, of dW: the tokens), rows of a bucket in pieces, the last ones ragged
             (96, 72, 1040, 2, 16, "mixed"), (2056, 64, 40, 2, 16, "mixed"), (3001, 136, 72, 1, 40, "last"), (1500, 64, 1032, 0, 0, "none"),
-            (4100, 72, 40, 70, 24, "last"), (5003, 64, 72, 131, 8, "ends")]
+            (4100, 72, 40, 70, 24, "last"), (5003, 64, 72, 131, 8, "ends"),
+            (515, 520, 264, 70, 40, "mixed"), (4100, 136, 584, 67, 40, "ends")]   # wavefronts by columns
 
 
 @pytest.mark.parametrize("N,d_in,F,C,rank,how,act", [c + (ACTS[i % 3],) for i, c in enumerate(BACKWARD)])
