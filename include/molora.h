@@ -480,7 +480,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * projections are one of the sum of their ranks, B block-diagonal).  z DEVICE bf16 [N][F] is ready to be
  * the x of a down projection.  h is stored only where pre (DEVICE fp32 [N][2 F], may be NULL) asks for
  * it, for the backward pass; without, z is made from the sums in the GEMM's registers, and a batch too small
- * to occupy the GPU keeps partial sums in the workspace (at most 32 MB).
+ * to occupy the GPU keeps partial sums in the workspace.
  * Without adapters: A, B, r NULL, C = rank = 0.  act: MOLORA_ACT_*.  F >= 8 and a multiple of 8; x, W
  * and h in bf16 below 4 GiB each.  workspace DEVICE, 256-byte aligned, of
  * molora_apply_gated_workspace_bytes(...) bytes, which never decrease with N.  Errors as molora_apply.

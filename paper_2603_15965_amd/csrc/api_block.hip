@@ -100,7 +100,7 @@ inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F
     }
     if (N <= kDecode) {
         const size_t plane = size_t(N) * 2 * F * 4;
-        w.slices = molora::small_base_slices(N, d_in, 2 * F, C);
+        w.slices = molora::small_base_slices_rounds(N, d_in, 2 * F, C);
         w.base = c.take<float>(plane);
         if (w.slices > 1) w.planes = c.take<float>(plane * (w.slices - 1));
     } else {

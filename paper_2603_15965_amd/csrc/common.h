@@ -257,6 +257,7 @@ hipError_t launch_small_shrink_base(const uint16_t *x, const uint16_t *W, const 
 // [slices - 1][N][d_out] (fp32), which launch_small_expand then adds; 1: K is not cut
 int small_base_ksplit(int64_t N, int d_in, int d_out, int C, int rank);
 int small_base_slices(int64_t N, int d_in, int d_out, int C);  // whatever the rank; C = 0: no adapters
+int small_base_slices_rounds(int64_t N, int d_in, int d_out, int C);  // also where the columns take several rounds
 // W for launch_small_shrink_base(..., w_packed = true): slabs of 16 rows, inside a slab groups of
 // gc = small_pack_cols(d_out) columns one after the other (0: this d_out has no packed form)
 int small_pack_cols(int d_out);

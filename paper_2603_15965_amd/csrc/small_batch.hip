@@ -1000,6 +1000,29 @@ int small_base_slices(int64_t N, int d_in, int d_out, int C) {
     return (int)ks;
 }
 
+// The same with more column groups than compute units, each of which holds one workgroup: the last round is short of
+// workgroups, and one by itself draws no more than 30 GB/s.  Time of the rounds in us: a start and an end, and the larger
+// of all their bytes of W at 5.5 TB/s and one workgroup's; the slices' sums are written and read once more.  64 x 4096 ->
+// 20480, 16 adapters of rank 64 76 -> 71 us for the gated block's step, 7 x 8192 -> 18432 93 -> 76, 30 x 4096 -> 18432 55
+// -> 49; 64 x 4096 -> 24576 stays whole (79, in two slices 87).
+int small_base_slices_rounds(int64_t N, int d_in, int d_out, int C) {
+    const int64_t groups = (d_out + 63) / 64;
+    if (N < 1 || N > 64 || groups <= 256) return small_base_slices(N, d_in, d_out, C);
+    int pick = 1;
+    double best = 1e30;
+    for (int ks = 1; ks <= 4 && (ks == 1 || ks * N * d_out <= kMaxPlaneFloats); ++ks) {
+        const double bytes = 128.0 * d_in / ks;
+        const int64_t full = groups * ks / 256, rest = groups * ks % 256;
+        const double last = rest > 0 ? fmax(rest * bytes / 5.5e6, bytes / 3e4) + 4 : 0;
+        const double cost = full * (256 * bytes / 5.5e6 + 4) + last + (ks - 1) * (double)(N * d_out) * 8 / 5e6;
+        if (cost < best) {
+            best = cost;
+            pick = ks;
+        }
+    }
+    return pick;
+}
+
 // N <= 64: dispatch + shrink + h = x W in one launch (sort.r, sort.offsets, sort.perm required)
 hipError_t launch_small_shrink_base(const uint16_t *x, const uint16_t *W, const uint16_t *A, float *h,
                                     uint16_t *t_out, int64_t N, int d_in, int d_out, int C, int rank,

@@ -50,7 +50,7 @@ def _guarded(torch, shape, dtype, fill=7.0):
 FORWARD = [(1, 64, 8, 1, 8, "last"), (1, 512, 264, 4, 16, "mixed"), (7, 136, 40, 3, 16, "mixed"), (33, 264, 72, 5, 24, "mixed"),
            (64, 256, 136, 6, 64, "mixed"), (64, 128, 24, 3, 128, "none"), (65, 64, 8, 1, 8, "last"), (66, 136, 40, 3, 16, "mixed"),
            (130, 264, 200, 5, 40, "mixed"), (300, 520, 264, 64, 16, "mixed"), (515, 1032, 328, 7, 24, "mixed"), (600, 72, 520, 2, 128, "mixed"),
-           (1, 64, 24, 0, 0, "none"), (40, 264, 136, 0, 0, "none"), (200, 136, 264, 0, 0, "none")]
+           (5, 2056, 8328, 3, 16, "mixed"), (1, 64, 24, 0, 0, "none"), (40, 264, 136, 0, 0, "none"), (200, 136, 264, 0, 0, "none")]
 
 
 @pytest.mark.parametrize("act", ACTS)
