@@ -214,3 +214,39 @@ def test_apply_mx_many_buckets_in_large_tiles():
     want, off = _product_ref(w.x, w.W)
     l, lo = ref.lora(ref.f64(w.x), ref.f64(w.A), ref.f64(w.B), r)
     assert (np.abs(h - want - l) <= off + lo + 2 * ref.ULP32 * (np.abs(l) + np.abs(want))).all()
+
+
+def test_offsets_beyond_32_bits():
+    """x of more than 4 GiB: the last rows as by themselves (codes the same, sums in another order)."""
+    torch, mb = _gpu()
+    N, d_in, d_out, C, rank, tail = 266256, 8200, 40, 3, 8, 112
+    print(f"x {N} x {d_in}, {N * d_in * 2 / 2 ** 30:.2f} GiB", flush=True)
+    torch.manual_seed(11)
+    x = torch.empty(N, d_in, dtype=torch.bfloat16, device="cuda")
+    for lo in range(0, N, 32768):
+        x[lo:lo + 32768].normal_()
+    W = (torch.randn(d_in, d_out, device="cuda") / d_in ** 0.5).bfloat16()
+    A = (torch.randn(C, d_in, rank, device="cuda") / d_in ** 0.5).bfloat16()
+    B = (torch.randn(C, rank, d_out, device="cuda") / rank ** 0.5).bfloat16()
+    r = (torch.arange(N, device="cuda") % (C + 1)).to(torch.int32)   # one in four without adapter
+    wc, ws = mb.molora_mx_quantize_w(W)
+    assert N % 16 == 0 and tail % 16 == 0
+    codes, scales = mb.molora_mx_quantize(x)
+    c2, s2 = mb.molora_mx_quantize(x[-tail:])
+    assert torch.equal(codes[-tail // 16:], c2) and torch.equal(scales[-tail // 16:], s2)
+    h = mb.molora_mx_matmul(codes, scales, wc, ws, N, d_in, d_out)[-tail:]
+    one = mb.molora_mx_matmul(c2, s2, wc, ws, tail, d_in, d_out)
+    qx, qw = mb.molora_mx_dequantize(c2, s2, tail, d_in).abs().double(), mb.molora_mx_dequantize(wc, ws, d_out, d_in).abs().double()
+    # two fp32 sums of d_in terms, each addition off by half a step
+    off = 2 * d_in * 2.0 ** -24 * (qx @ qw.t().contiguous())
+    assert bool(((h.double() - one.double()).abs() <= off).all())
+    del codes, scales
+    h = mb.molora_apply_mx(x, wc, ws, A, B, r)[-tail:]
+    one = mb.molora_apply_mx(x[-tail:], wc, ws, A, B, r[-tail:])
+    low = torch.zeros(tail, d_out, dtype=torch.float64, device="cuda")
+    for c in range(C):
+        mine = r[-tail:] == c
+        low[mine] = x[-tail:][mine].double().abs() @ A[c].double().abs() @ B[c].double().abs()
+    # t is a sum of d_in terms, carried as two bf16 halves (2^-17 together); then rank terms beside the others
+    off += (2 * (d_in + 2 * rank) * 2.0 ** -24 + 2.0 ** -16) * low + 2 * 2 * rank * 2.0 ** -24 * (qx @ qw.t().contiguous())
+    assert bool(((h.double() - one.double()).abs() <= off).all())
