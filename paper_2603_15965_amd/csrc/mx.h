@@ -15,8 +15,6 @@
 namespace molora {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 inline __host__ __device__ int64_t mx_row_tiles(int64_t rows) { return (rows + 15) / 16; }
 inline __host__ __device__ int mx_k_tiles(int K) { return (int)(((int64_t)K + 127) / 128); }
