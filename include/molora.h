@@ -35,7 +35,8 @@
  *  - Data-dependent problems (a routing target outside [0, C)) cannot be seen by the
  *    host without a synchronisation; they are reported through an optional DEVICE flag
  *    and handled as "this token has no adapter" (see molora_bucket).
- *  - Inputs are expected to be finite.  The argmax is a scan from target 0 that moves on a
+ *  - Inputs are expected to be finite.  (molora_apply_mx and the gated block say what holds where they are
+ *    not.)  The argmax is a scan from target 0 that moves on a
  *    strict ">": a NaN logit at a target above 0 is never selected, a NaN at target 0 is
  *    kept unless a later logit compares greater (never, against NaN), so it yields r = 0.
  *    molora_route and molora_route_mlp take 2 to 3 times as long where x, G or W1 holds a NaN or
@@ -453,6 +454,8 @@ molora_status molora_apply_mix(const void *x, const void *W, const void *A, cons
  *                        x is given in bf16: the base product takes its 4-bit blocks (made inside), the
  *                        adapters x itself.  workspace as for molora_apply, of
  *                        molora_apply_mx_workspace_bytes(...) bytes, which never decrease with N.
+ *                        What is not finite in a row of x reaches that row of h, what is not in an adapter's A or B
+ *                        the rows of its tokens (each takes twice the time where it occurs), no others.
  * All pointers DEVICE, 16-byte aligned (workspace 256).  Errors as molora_apply.
  */
 size_t molora_mx_codes_bytes(int64_t rows, int32_t K);
@@ -495,6 +498,9 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * sums; a NULL one is not computed (dA and dB have to be NULL without adapters).  dh is rounded to
  * bf16 before these products.  workspace as above, of
  * molora_gated_backward_workspace_bytes(...) bytes, which never decrease with N.
+ *
+ * Infinities and NaN in the A or B of an adapter reach the rows of z, pre and dx of its tokens and its own dA and
+ * dB, nothing else; workgroups that meet them take twice the time.
  */
 size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank);
 molora_status molora_apply_gated(const void *x, const void *W, const void *A, const void *B,

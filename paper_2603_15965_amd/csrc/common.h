@@ -33,6 +33,27 @@ __device__ __forceinline__ i16x4 lds_read_tr16(const MOLORA_LDS void *p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((MOLORA_LDS i16x4 *)p);
 }
 
+// Products with one adapter's B take rows of other adapters along as zeros, and zero times an infinity or a NaN in B is
+// NaN.  The kernels that keep such values to the adapter's own rows look at their sums at the end, and a workgroup
+// where one is not finite computes them once more (CAREFUL), every row with its own adapter's products alone.
+// Choosing in the first place costs an instruction per register of every product: 2 to 7 % of a call with many
+// adapters, 15 % in the streaming kernel.
+template <class V>
+__device__ __forceinline__ void find_not_finite(float &seen, const V &v) {  // seen: 0, NaN from the first such value on
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(V) / sizeof(float)); ++i) seen = __builtin_fmaf(v[i], 0.f, seen);
+}
+
+// The thread's index, new to the compiler at every call: what the first computation derives from it is not kept in
+// registers for the second one.  (Without its range an expand with 256 buckets takes 12 % longer.)
+template <int THREADS>
+__device__ __forceinline__ int fresh_thread() {
+    int t = (int)threadIdx.x;
+    asm volatile("" : "+v"(t));
+    __builtin_assume(t >= 0 && t < THREADS);
+    return t;
+}
+
 // How a bucket maps to adapters (weighted top-k mixture of Sec. "Router Architecture", slot
 // table of Def. "Hot-Set Layout").  Bucket b stands for the ordered tuple of k adapters
 // c_j = (b / C^j) % C, j < k; adapter c lives in position slots[c] of the A / B pools
@@ -245,6 +266,10 @@ hipError_t launch_small_batch_gemm(const uint16_t *x, const uint16_t *W, const u
                                    const uint16_t *t2, const int32_t *offsets, const int32_t *perm,
                                    float *h, int64_t N, int d_in, int d_out, int C, int rank, Mix mix,
                                    hipStream_t s);
+// The same for more than 64 tokens; infinities and NaN in an adapter's B reach its own rows only
+hipError_t launch_small_batch_gemm_own_rows(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                                            const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in,
+                                            int d_out, int C, int rank, hipStream_t s);
 // A batch of at most 64 tokens in two launches instead of four: (1) the dispatch step, the shrink
 // and the base projection h = x W side by side (the latency-bound shrink hides behind the
 // stream of W), (2) the expand added to h.

@@ -217,6 +217,11 @@ __device__ __forceinline__ bf16x8 t_operand(const unsigned char *t_lds, int i, i
     if (!(tokens >> row & 1) || kc >= R) v = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
     return __builtin_bit_cast(bf16x8, v);
 }
+// What a lane keeps of a product with the B of an adapter whose tokens these are: row tile i's sum for a row of the
+// adapter, what was there before for any other
+__device__ __forceinline__ f32x4 own_row(uint64_t tokens, int i, int lane, f32x4 sum, f32x4 before) {
+    return tokens >> (i * 16 + (lane & 15)) & 1 ? sum : before;
+}
 // the columns [16] x 8 k of a slab that lies k-row by k-row in LDS, k-rows 8 kg .. 8 kg + 7 from p on
 __device__ __forceinline__ bf16x8 turned(const unsigned char *slab, int stride, int kg, int col_bytes, int lane) {
     const unsigned char *p = slab + (kg * 8 + ((lane & 15) >> 2)) * stride + col_bytes + (lane & 3) * 8;

@@ -26,18 +26,19 @@ struct FinishLds {
 // A workgroup owns the same CT * 16 columns of the gate and of the up half, so that both factors of a z meet in it.  Its
 // eight wavefronts take slabs of 16 rows of the B_c in use in turn, in token order (decode_body.h), and add their sums
 // in LDS in a fixed order.
-template <int NR, int CT>
-__global__ __launch_bounds__(512, 2) void gated_finish_kernel(const float *base, const float *__restrict__ planes,
-                                                              int slices, const uint16_t *__restrict__ B,
-                                                              const int32_t *__restrict__ r, const uint16_t *__restrict__ t2,
-                                                              const int32_t *__restrict__ perm, uint16_t *__restrict__ z,
-                                                              float *pre, int N, int F, int C, int R, int act) {
+// (false: a sum is not finite, nothing is stored; CAREFUL: common.h, find_not_finite)
+template <int NR, int CT, bool CAREFUL>
+__device__ __forceinline__ bool gated_finish_body(const float *base, const float *__restrict__ planes, int slices,
+                                                  const uint16_t *__restrict__ B, const int32_t *__restrict__ r,
+                                                  const uint16_t *__restrict__ t2, const int32_t *__restrict__ perm,
+                                                  uint16_t *__restrict__ z, float *pre, int N, int F, int C, int R, int act,
+                                                  int *not_finite) {
     using Lds = FinishLds<NR, CT>;
     constexpr int CPR = Lds::CPR, STRIDE = Lds::STRIDE;
     constexpr int BL = (16 * CPR + 63) / 64, BATCH = CT < 4 ? 4 : 2;  // loads of a slab, slabs of a wavefront in flight
     constexpr int OUTS = (CT * NR + 7) / 8;              // 16 x 16 tiles of z per wavefront
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = fresh_thread<512>(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kq = lane >> 4, l16 = lane & 15;
     const int n0 = (int)blockIdx.x * (CT * 16);
     const int64_t pitch = 2 * (int64_t)F;
@@ -118,7 +119,10 @@ __global__ __launch_bounds__(512, 2) void gated_finish_kernel(const float *base,
                 for (int j = 0; j < 2 * CT; ++j) {
                     const bf16x8 fb = turned(slab, STRIDE, kq & 1, j * 32, lane);
 #pragma unroll
-                    for (int i = 0; i < NR; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb, t[i], acc[j][i], 0, 0, 0);
+                    for (int i = 0; i < NR; ++i) {
+                        const f32x4 all = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb, t[i], acc[j][i], 0, 0, 0);
+                        acc[j][i] = CAREFUL ? own_row(tokens, i, lane, all, acc[j][i]) : all;
+                    }
                 }
             }
         }
@@ -141,18 +145,28 @@ __global__ __launch_bounds__(512, 2) void gated_finish_kernel(const float *base,
         __syncthreads();
     }
 
+    if (C > 0) {
+        float seen = 0.f;
 #pragma unroll
-    for (int o = 0; o < OUTS; ++o) {
-        const int f = wave + o * 8;
-        if (f >= CT * NR) break;
-        const int row = f % NR * 16 + l16, col = n0 + f / NR * 16 + kq * 4;
-        if (C > 0) {
+        for (int o = 0; o < OUTS; ++o) {
+            const int f = min(wave + o * 8, CT * NR - 1);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) sum[o][half] += *(const f32x4 *)(lds + v * Lds::PART + (half * CT * NR + f) * 1024 + lane * 16);
+                find_not_finite(seen, sum[o][half]);
+            }
         }
-        if (row < N && col < F) {
+        if (!CAREFUL) {  // (before anything is stored: base may be pre)
+            if (seen != 0.f) *not_finite = 1;
+            __syncthreads();
+            if (*not_finite != 0) return false;
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < OUTS; ++o) {
+        const int f = wave + o * 8, row = f % NR * 16 + l16, col = n0 + f / NR * 16 + kq * 4;
+        if (f < CT * NR && row < N && col < F) {
             if (pre != nullptr) {
                 *(f32x4 *)(pre + row * pitch + col) = sum[o][0];
                 *(f32x4 *)(pre + row * pitch + F + col) = sum[o][1];
@@ -160,6 +174,19 @@ __global__ __launch_bounds__(512, 2) void gated_finish_kernel(const float *base,
             *(u32x2 *)(z + (int64_t)row * F + col) = bf16x4_bits(gate4(sum[o][0], sum[o][1], act));
         }
     }
+    return true;
+}
+
+template <int NR, int CT>
+__global__ __launch_bounds__(512, 2) void gated_finish_kernel(const float *base, const float *__restrict__ planes,
+                                                              int slices, const uint16_t *__restrict__ B,
+                                                              const int32_t *__restrict__ r, const uint16_t *__restrict__ t2,
+                                                              const int32_t *__restrict__ perm, uint16_t *__restrict__ z,
+                                                              float *pre, int N, int F, int C, int R, int act) {
+    __shared__ int not_finite;
+    if (threadIdx.x == 0) not_finite = 0;  // (a barrier follows before it is set)
+    if (!gated_finish_body<NR, CT, false>(base, planes, slices, B, r, t2, perm, z, pre, N, F, C, R, act, &not_finite))
+        gated_finish_body<NR, CT, true>(base, planes, slices, B, r, t2, perm, z, pre, N, F, C, R, act, nullptr);
 }
 
 template <int NR, int CT>

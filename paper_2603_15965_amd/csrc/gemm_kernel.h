@@ -97,6 +97,9 @@ enum GemmOut {
     kOutPlanes, // h of one slice of K (blockIdx.y), fp32, to the slice's plane
     kOutGated,  // z = act(gate half of h) * up half of h, bf16, and h itself where it is wanted
 };
+// Does what one adapter's B holds reach its own rows only?  (h in fp32 wants finite inputs; bf16 from a W by rows of k is the
+// weight's gradient, which has no adapters.)
+constexpr bool gemm_own_rows(int out, bool wt) { return out != kOutF32 && (out != kOutBf16 || wt); }
 struct GemmEpilogue {
     uint16_t *out16 = nullptr;  // bf16 h, or z
     int act = 0;                // kOutGated: the activation
@@ -108,14 +111,16 @@ struct GemmEpilogue {
 // WT: W is given as [d_out][d_in], rows of k, the way a gradient meets the weight of its product: its tile lies in LDS as
 // the x tile does, and its fragments are read the same way (with W turned by a launch of its own a step of
 // 106 x 3680 -> 2 x 6208 took 30 us more).
-template <class Cfg, int OUT = kOutF32, bool WT = false>
-__global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
+// (false: a sum is not finite; CAREFUL: common.h, find_not_finite)
+template <class Cfg, int OUT, bool WT, bool CAREFUL>
+__device__ __forceinline__ bool fused_gemm_body(
     const uint16_t *__restrict__ x, const uint16_t *__restrict__ W, const uint16_t *__restrict__ B,
     const uint16_t *__restrict__ t2, const int32_t *__restrict__ offsets,
     const int32_t *__restrict__ perm, float *__restrict__ h, int N, int d_in, int d_out, int C,
     int rank, int tiles_m, int tiles_n, Mix mix, GemmEpilogue ep) {
     constexpr int BM = Cfg::BM, BN = Cfg::BN, BK = Cfg::BK, NT = Cfg::NT, TM = Cfg::TM,
                   TN = Cfg::TN, STAGES = Cfg::STAGES;
+    constexpr bool OWN = gemm_own_rows(OUT, WT);
     // (1 KB alignment: the operand reads XOR k-step bits into addresses relative to this base)
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     int32_t *tile_perm = (int32_t *)(smem + STAGES * Cfg::STAGE);  // [BM] token per row, -1 = none
@@ -134,7 +139,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         h += (int64_t)blockIdx.y * N * d_out;
         d_in = min(ep.k_slice, d_in - k0);
     }
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = OWN ? fresh_thread<Cfg::NT>() : (int)threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
 
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     const int share = (total - whole * 8 + 7) / 8;
     const int logical = in_xcd < whole ? (in_xcd / kXcdRun * 8 + xcd) * kXcdRun + in_xcd % kXcdRun
                                        : whole * 8 + xcd * share + in_xcd - whole;
-    if (logical >= total) return;
+    if (logical >= total) return true;
     // Group g holds the row tiles g, g + ng, g + 2 ng, ... (at most kGroupM of them), not
     // kGroupM consecutive ones: the rows are gathered through perm, so consecutive row tiles
     // share nothing, but under a skewed routing the LAST row tiles are the ones crossed by many
@@ -288,6 +293,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
         return perm[p];
     };
     if (tid == 0) *nseg_p = 0;
+    if (OWN && tid == 0) nseg_p[1] = 0;
     int32_t my_tok = -1, o_lo = 0, o_hi = 0;
     if (tid < BM && row_pos(tid) < N) my_tok = token_at(row_pos(tid));
     if (tid < C) {
@@ -457,7 +463,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
     // loop is unrolled by their number, so each copy knows its stage and reads through the constants in
     // `at`; elsewhere the stage offset is added once per tile.  (Three stages, formed per tile and unrolled: 655 x
     // 8888 -> 10624 146 -> 133 us, 2464 x 11720 -> 2304 176 -> 171, 635 x 8192 -> 2048 42.7 -> 42.1.)
-    constexpr bool kUnrolled = STAGES <= 3;
+    constexpr bool kUnrolled = STAGES <= 3 && !CAREFUL;
     Addr at[kUnrolled ? STAGES : 1], cur_rt, nxt_rt;
 #pragma unroll
     for (int st = 0; st < (kUnrolled ? STAGES : 1); ++st) {  // (opaque: as a sum it is formed again for every read)
@@ -700,10 +706,26 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
                     const int p = pr + u * 16 + l16;
                     const i16x8 own = p >= lo && p < hi ? t[u] : i16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                    for (int tn = 0; tn < TN; ++tn)
-                        acc[2 * k + u][tn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[tn], __builtin_bit_cast(bf16x8, own), acc[2 * k + u][tn], 0, 0, 0);
+                    for (int tn = 0; tn < TN; ++tn) {
+                        const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[tn], __builtin_bit_cast(bf16x8, own), acc[2 * k + u][tn], 0, 0, 0);
+                        acc[2 * k + u][tn] = !CAREFUL || (p >= lo && p < hi) ? sum : acc[2 * k + u][tn];
+                    }
                 }
             }
+        }
+    }
+
+    // a sum that is not finite, in a tile that one bucket does not fill
+    bool look = false;
+    if constexpr (OWN && !CAREFUL) {
+        look = nseg > 0 && !(nseg == 1 && seg_lo[0] <= blk0 && seg_hi[0] >= min(blk_pos(BM / 32 - 1) + 32, N));
+        if (look) {
+            float seen = 0.f;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) find_not_finite(seen, acc[i][j]);
+            if (seen != 0.f) nseg_p[1] = 1;
         }
     }
 
@@ -796,6 +818,21 @@ __global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
                 }
             }
         }
+    }
+    return !look || nseg_p[1] == 0;  // (barriers lie behind the one that set it)
+}
+
+template <class Cfg, int OUT = kOutF32, bool WT = false>
+__global__ __launch_bounds__(Cfg::NT, 2) void fused_gemm_kernel(
+    const uint16_t *__restrict__ x, const uint16_t *__restrict__ W, const uint16_t *__restrict__ B,
+    const uint16_t *__restrict__ t2, const int32_t *__restrict__ offsets,
+    const int32_t *__restrict__ perm, float *__restrict__ h, int N, int d_in, int d_out, int C,
+    int rank, int tiles_m, int tiles_n, Mix mix, GemmEpilogue ep) {
+    const bool done = fused_gemm_body<Cfg, OUT, WT, false>(x, W, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, tiles_m, tiles_n, mix, ep);
+    if constexpr (gemm_own_rows(OUT, WT)) {
+        if (done) return;
+        __syncthreads();  // nothing in LDS is read any more
+        fused_gemm_body<Cfg, OUT, WT, true>(x, W, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, tiles_m, tiles_n, mix, ep);
     }
 }
 

@@ -19,7 +19,7 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
     int count = 1;
     const hipError_t e =
         pick.config < 0
-            ? launch_small_batch_gemm(x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, Mix{1, C, nullptr, nullptr}, s)
+            ? launch_small_batch_gemm_own_rows(x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, s)
             : launch_planes<false>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, count, s);
     return e != hipSuccess ? e : launch_gate(planes, count, z, pre, N, F, act, s);
 }

@@ -43,17 +43,18 @@ struct DecodeLds {
     static constexpr int bytes(int R) { return 8 * PART + NR * 16 * t_row_bytes(R); }
 };
 
-template <int NR, int CT>
-__global__ __launch_bounds__(512, 2) void mx_decode_kernel(const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs,
-                                                           const uint8_t *__restrict__ wc, const uint8_t *__restrict__ ws,
-                                                           const uint16_t *__restrict__ B, const int32_t *__restrict__ r,
-                                                           const float *__restrict__ planes, float *__restrict__ h, int N, int d_out,
-                                                           int kt_n, int kg_n, int C, int R, int slices) {
+// (false: a sum is not finite; CAREFUL: common.h, find_not_finite)
+template <int NR, int CT, bool CAREFUL>
+__device__ __forceinline__ bool mx_decode_body(const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs,
+                                               const uint8_t *__restrict__ wc, const uint8_t *__restrict__ ws,
+                                               const uint16_t *__restrict__ B, const int32_t *__restrict__ r,
+                                               const float *__restrict__ planes, float *__restrict__ h, int N, int d_out, int kt_n,
+                                               int kg_n, int C, int R, int slices, int *not_finite) {
     using Lds = DecodeLds<NR, CT>;
     constexpr int STRIDE = Lds::STRIDE, LPR = CT * 2, LOADS = (16 * LPR + 63) / 64;  // 16-byte chunks of a row, loads of a slab
     constexpr int BATCH = 4;  // slabs of a wavefront in flight
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = fresh_thread<512>(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kq = lane >> 4, l16 = lane & 15;
     const int64_t ct0 = (int64_t)blockIdx.x * CT, ct_last = (d_out + 15) / 16 - 1, n0 = ct0 * 16;
     unsigned char *const t_lds = lds + 8 * Lds::PART;
@@ -157,7 +158,10 @@ __global__ __launch_bounds__(512, 2) void mx_decode_kernel(const uint8_t *__rest
                 for (int j = 0; j < CT; ++j) {
                     const bf16x8 fb = turned(slab, STRIDE, kq & 1, j * 32, lane);
 #pragma unroll
-                    for (int i = 0; i < NR; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb, t[i], acc[j][i], 0, 0, 0);
+                    for (int i = 0; i < NR; ++i) {
+                        const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb, t[i], acc[j][i], 0, 0, 0);
+                        acc[j][i] = CAREFUL ? own_row(mine, i, lane, sum, acc[j][i]) : sum;
+                    }
                 }
             }
         }
@@ -168,6 +172,7 @@ __global__ __launch_bounds__(512, 2) void mx_decode_kernel(const uint8_t *__rest
 #pragma unroll
         for (int i = 0; i < NR; ++i) *(f32x4 *)(lds + wave * Lds::PART + ((j * NR + i) * 64 + lane) * 16) = acc[j][i];
     __syncthreads();
+    float seen = 0.f;
     for (int f = wave; f < CT * NR; f += 8) {
         f32x4 sum = *(const f32x4 *)(lds + (f * 64 + lane) * 16);
 #pragma unroll
@@ -175,7 +180,24 @@ __global__ __launch_bounds__(512, 2) void mx_decode_kernel(const uint8_t *__rest
         const int row = f % NR * 16 + l16;
         const int64_t col = (ct0 + f / NR) * 16 + kq * 4;
         if (row < N && col < d_out) *(f32x4 *)(h + (int64_t)row * d_out + col) = sum;
+        find_not_finite(seen, sum);
     }
+    if (CAREFUL || C == 0) return true;
+    if (seen != 0.f) *not_finite = 1;
+    __syncthreads();
+    return *not_finite == 0;
+}
+
+template <int NR, int CT>
+__global__ __launch_bounds__(512, 2) void mx_decode_kernel(const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs,
+                                                           const uint8_t *__restrict__ wc, const uint8_t *__restrict__ ws,
+                                                           const uint16_t *__restrict__ B, const int32_t *__restrict__ r,
+                                                           const float *__restrict__ planes, float *__restrict__ h, int N, int d_out,
+                                                           int kt_n, int kg_n, int C, int R, int slices) {
+    __shared__ int not_finite;
+    if (threadIdx.x == 0) not_finite = 0;  // (a barrier follows before it is set)
+    if (!mx_decode_body<NR, CT, false>(xc, xs, wc, ws, B, r, planes, h, N, d_out, kt_n, kg_n, C, R, slices, &not_finite))
+        mx_decode_body<NR, CT, true>(xc, xs, wc, ws, B, r, planes, h, N, d_out, kt_n, kg_n, C, R, slices, nullptr);
 }
 
 template <int NR, int CT>

@@ -41,8 +41,9 @@ struct MxCfg {
     static_assert(NW * 16 * OUT_STRIDE <= STAGES * STAGE, "the epilogue fits the stages");
 };
 
-template <class Cfg>
-__global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
+// (false: a sum is not finite; CAREFUL: common.h, find_not_finite)
+template <class Cfg, bool CAREFUL>
+__device__ __forceinline__ bool mx_gemm_body(
     const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs, const uint8_t *__restrict__ wc,
     const uint8_t *__restrict__ ws, const uint16_t *__restrict__ B, const uint16_t *__restrict__ t2,
     const int32_t *__restrict__ offsets, const int32_t *__restrict__ perm, float *__restrict__ h, int N, int d_out,
@@ -50,14 +51,14 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
     constexpr int TM = Cfg::TM, TN = Cfg::TN, RT = Cfg::RT, NW = Cfg::NW, STAGES = Cfg::STAGES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     unsigned char *const scales = smem + STAGES * Cfg::STAGE;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = fresh_thread<Cfg::NT>(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
 
     // XCDs take runs of tiles, eight row tiles wide, so that each one's L2 holds its rows and columns
     const int total = tiles_m * tiles_n, share = (total + 7) / 8;
     const int logical = (int)(blockIdx.x % 8) * share + (int)(blockIdx.x / 8);
-    if (blockIdx.x / 8 >= (unsigned)share || logical >= total) return;
+    if (blockIdx.x / 8 >= (unsigned)share || logical >= total) return true;
     const int group = logical / (8 * tiles_n), first = group * 8;
     const int width = min(8, tiles_m - first), in_group = logical - first * tiles_n;
     const int tile_m = first + in_group % width, tile_n = in_group / width;
@@ -235,7 +236,11 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
 #pragma unroll
         for (int j = 0; j < TN; ++j) sw[j] >>= 8;
     }
-    __syncthreads();  // the stages are free
+    // a tile that buckets have rows of, but no bucket all
+    const bool look = !CAREFUL && c_first < C && !(lo_first <= p0 && hi_first >= min(p0 + Cfg::BM, N));
+    int *const not_finite = (int *)scales;
+    __syncthreads();  // the stages and the scales are free
+    if (look && tid == 0) *not_finite = 0;  // (a barrier follows before it is set)
 
     // ---- expand: the buckets that own rows of the tile, 32 columns of t at a time ----
     // A fragment of 32 k is [hi | lo] of 16 columns of t against the same 16 rows of B twice.  The next step's rows of
@@ -263,7 +268,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
                 for (int u = 0; u < 2; ++u) {
                     const int kc = k0 + u * 16 + (kq & 1) * 8;
                     t[u][i] = *(const i16x8 *)(row + min(kc, R - 8));
-                    if (p < lo || p >= hi || kc >= R) t[u][i] = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    if ((!CAREFUL && (p < lo || p >= hi)) || kc >= R) t[u][i] = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
                 }
             }
         };
@@ -306,10 +311,20 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
                     const int first_row = p0 + (wm * TM + i) * 16;
                     if (hi_now <= first_row || lo_now >= first_row + 16) continue;
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], __builtin_bit_cast(bf16x8, t[u][i]), acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < TN; ++j) {
+                        const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], __builtin_bit_cast(bf16x8, t[u][i]), acc[i][j], 0, 0, 0);
+                        acc[i][j] = !CAREFUL || (uint32_t)(l16 + (first_row - lo_now)) < (uint32_t)(hi_now - lo_now) ? sum : acc[i][j];
+                    }
                 }
             }
+        }
+        if (look) {
+            float seen = 0.f;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) find_not_finite(seen, acc[i][j]);
+            if (seen != 0.f) *not_finite = 1;
         }
         __syncthreads();
     }
@@ -333,6 +348,18 @@ __global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
             }
         }
     }
+    return !look || *not_finite == 0;
+}
+
+template <class Cfg>
+__global__ __launch_bounds__(Cfg::NT, 2) void mx_gemm_kernel(
+    const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs, const uint8_t *__restrict__ wc,
+    const uint8_t *__restrict__ ws, const uint16_t *__restrict__ B, const uint16_t *__restrict__ t2,
+    const int32_t *__restrict__ offsets, const int32_t *__restrict__ perm, float *__restrict__ h, int N, int d_out,
+    int kt_n, int kg_n, int C, int R, int tiles_m, int tiles_n) {
+    if (mx_gemm_body<Cfg, false>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_out, kt_n, kg_n, C, R, tiles_m, tiles_n)) return;
+    __syncthreads();  // nothing in LDS is read any more
+    mx_gemm_body<Cfg, true>(xc, xs, wc, ws, B, t2, offsets, perm, h, N, d_out, kt_n, kg_n, C, R, tiles_m, tiles_n);
 }
 
 template <class Cfg>

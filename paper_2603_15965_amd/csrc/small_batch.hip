@@ -127,6 +127,9 @@ inline int sorted_places(int N, int C, int groups, int others) {
 }
 constexpr int kSbBaseSplit = 8;  // most K slices of a base projection
 constexpr int kSbBaseOnly = 1, kSbExpandOnly = 2, kSbBasePacked = 3, kSbExpandPacked = 4, kSbExpandSum = 5;
+// mode 0 without mixture that reports sums that are not finite, and the same with every row's own adapter's products
+// alone (common.h: find_not_finite)
+constexpr int kSbOwnRows = 6, kSbOwnRowsCareful = 7;
 
 template <int TM, int TN, bool SHRINK, int MODE = 0, int NWV = kSbWaves>  // TM: 32-row blocks, 1 (N <= 32) or 2
 __device__ __forceinline__ void small_batch_body(
@@ -134,7 +137,7 @@ __device__ __forceinline__ void small_batch_body(
     const uint16_t *__restrict__ t2, const int32_t *__restrict__ offsets,
     const int32_t *__restrict__ perm, float *__restrict__ h, uint16_t *__restrict__ t_out, int N,
     int d_in, int d_out, int C, int rank, Mix mix, int ksplit, float *__restrict__ planes, SortArgs sort,
-    SbBlock wg) {
+    SbBlock wg, int *not_finite = nullptr) {
     using Geo = SbGeom<TN, NWV>;
     constexpr int kSbCols = Geo::COLS, kSbSlot = Geo::SLOT, kSbRowBytes = Geo::ROW_BYTES,
                   kSbWaveLds = Geo::WAVE_LDS;
@@ -146,7 +149,7 @@ __device__ __forceinline__ void small_batch_body(
     int32_t *nseg_p = seg_hi + 64;
     int32_t *seg_ad = nseg_p + 4;  // [64][4] pool positions of the adapters of a bucket's tuple
 
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = MODE == kSbOwnRows || MODE == kSbOwnRowsCareful ? fresh_thread<NWV * 64>() : (int)threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = wg.x * kSbCols;
     unsigned char *ring = smem + wave * kSbWaveLds;
@@ -616,14 +619,30 @@ __device__ __forceinline__ void small_batch_body(
                 bf16x8 bfr[TN];
 #pragma unroll
                 for (int tn = 0; tn < TN; ++tn) bfr[tn] = load_b_frag(ring + g * kSbSlot, tn);
+                int lo = 0, hi = 0;  // the bucket's rows in the tile
+                if constexpr (MODE == kSbOwnRowsCareful) {
+                    const int sg = (q0 + NWV * g) / nsl;
+                    lo = __builtin_amdgcn_readfirstlane(seg_lo[sg]) - row_base;
+                    hi = __builtin_amdgcn_readfirstlane(seg_hi[sg]) - row_base;
+                }
 #pragma unroll
                 for (int hl = 0; hl < 2; ++hl)
 #pragma unroll
                     for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
-                        for (int tn = 0; tn < TN; ++tn)
-                            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        for (int tn = 0; tn < TN; ++tn) {
+                            const f32x16 sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                                 ta[g][hl][tm], bfr[tn], acc[tm][tn], 0, 0, 0);
+                            if constexpr (MODE == kSbOwnRowsCareful) {
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) {  // (rows as below, where they are stored)
+                                    const int row = tm * 32 + (v >> 2) * 8 + kg * 4 + (v & 3);
+                                    acc[tm][tn][v] = row >= lo && row < hi ? sum[v] : acc[tm][tn][v];
+                                }
+                            } else {
+                                acc[tm][tn] = sum;
+                            }
+                        }
             }
             wait_lds();  // the slabs have been read before the next round refills them
         }
@@ -641,6 +660,7 @@ __device__ __forceinline__ void small_batch_body(
                 *(float *)(ring + row * kSbRowBytes + (tn * 32 + m_lo) * 4) = acc[tm][tn][v];
         }
     __syncthreads();
+    float seen = 0.f;
 #pragma unroll
     for (int j = 0; j < kOutIters; ++j) {
         const int it = tid + j * NWV * 64;
@@ -669,9 +689,13 @@ __device__ __forceinline__ void small_batch_body(
                     if (expand_sum && sl < ksplit) xw += h_old[j][sl];
                 sum += xw;
             }
+            if constexpr (MODE == kSbOwnRows) find_not_finite(seen, sum);
             float *dst = base_sliced && slice > 0 ? planes + (int64_t)(slice - 1) * N * d_out : h;
             *(f32x4 *)(dst + (int64_t)tok * d_out + col) = sum;
         }
+    }
+    if constexpr (MODE == kSbOwnRows) {
+        if (seen != 0.f) *not_finite = 1;
     }
 }
 
@@ -767,8 +791,19 @@ __global__ __launch_bounds__(NWV * 64) void small_batch_kernel(
             wg = SbBlock{(int)blockIdx.y, bucket, tile * ksplit + (int)blockIdx.z, C};
         }
     }
-    small_batch_body<TM, TN, SHRINK, MODE, NWV>(x, W, B, t2, offsets, perm, h, t_out, N, d_in, d_out, C, rank,
-                                                mix, ksplit, planes, sort, wg);
+    if constexpr (MODE == kSbOwnRows) {
+        __shared__ int not_finite;
+        if (threadIdx.x == 0) not_finite = 0;  // (a barrier follows before it is set)
+        small_batch_body<TM, TN, SHRINK, MODE, NWV>(x, W, B, t2, offsets, perm, h, t_out, N, d_in, d_out, C, rank,
+                                                    mix, ksplit, planes, sort, wg, &not_finite);
+        __syncthreads();
+        if (not_finite != 0)
+            small_batch_body<TM, TN, SHRINK, kSbOwnRowsCareful, NWV>(x, W, B, t2, offsets, perm, h, t_out, N, d_in, d_out,
+                                                                     C, rank, mix, ksplit, planes, sort, wg);
+    } else {
+        small_batch_body<TM, TN, SHRINK, MODE, NWV>(x, W, B, t2, offsets, perm, h, t_out, N, d_in, d_out, C, rank,
+                                                    mix, ksplit, planes, sort, wg);
+    }
 }
 
 // A decode-sized batch (N <= 64): the shrink (with the dispatch step inside, see SortArgs) and
@@ -865,7 +900,7 @@ hipError_t launch_small(const uint16_t *x, const uint16_t *W, const uint16_t *B,
     const dim3 grid = !SHRINK ? dim3(groups, row_tiles)
                               : (sort.r != nullptr && N <= 64 ? dim3(groups, (unsigned)sorted_places(N, C, (int)groups * ksplit, 0), (unsigned)ksplit)
                                                    : dim3(items, groups, (unsigned)ksplit));
-    if constexpr (!SHRINK && MODE == 0)  // the small-batch GEMM: base projection and expand
+    if constexpr (!SHRINK && (MODE == 0 || MODE == kSbOwnRows))  // the small-batch GEMM: base projection and expand
         launch_base_kernel(kern, grid, dim3(NWV * 64), Geo::LDS_BYTES, s, x, W, B, t2, offsets, perm, h,
                            t_out, N, d_in, d_out, C, rank, mix, ksplit, planes, sort);
     else
@@ -907,7 +942,9 @@ hipError_t launch_small_tn(const uint16_t *x, const uint16_t *W, const uint16_t 
             return launch_small<2, 1, true, 0, 4>(x, W, B, t2, offsets, perm, h, t_out, N, d_in, d_out, C, rank,
                                                   mix, s, ksplit, sort, planes);
     }
-    if constexpr (always_narrow) {
+    if constexpr (MODE == kSbOwnRows) {  // (more than 64 rows: checked by its launcher)
+        return narrow ? MOLORA_SB_LAUNCH(2, 1) : MOLORA_SB_LAUNCH(2, 2);
+    } else if constexpr (always_narrow) {
         return N <= 32 ? MOLORA_SB_LAUNCH(1, 1) : MOLORA_SB_LAUNCH(2, 1);
     } else {
         if (N <= 32) return narrow ? MOLORA_SB_LAUNCH(1, 1) : MOLORA_SB_LAUNCH(1, 2);
@@ -924,6 +961,13 @@ hipError_t launch_small_batch_gemm(const uint16_t *x, const uint16_t *W, const u
                                    hipStream_t s) {
     return launch_small_tn<false>(x, W, B, t2, offsets, perm, h, nullptr, (int)N, d_in, d_out, C, rank,
                                   mix, s);
+}
+hipError_t launch_small_batch_gemm_own_rows(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                                            const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in,
+                                            int d_out, int C, int rank, hipStream_t s) {
+    if (N <= 64) return hipErrorInvalidValue;
+    return launch_small_tn<false, kSbOwnRows>(x, W, B, t2, offsets, perm, h, nullptr, (int)N, d_in, d_out, C, rank,
+                                              Mix{1, C, nullptr, nullptr}, s);
 }
 
 namespace {
