@@ -732,12 +732,22 @@ def _mx_shapes(rows, K):
     return (tiles, -(-K // 128), 64, 16), (tiles, -(-K // 512), 64, 4)
 
 
-def _mx_outputs(rows, K, codes, scales, like):
+def _empty(shape, dtype, device, stream):
+    """What a call on `stream` writes and the caller did not hand in, from that stream's memory (as under
+    torch.cuda.stream(stream)): a block of the current stream may still be in use by kernels there that nothing
+    orders before this call's, and given back early it would go to kernels that nothing orders behind them."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _mx_outputs(rows, K, codes, scales, like, stream):
     c, s = _mx_shapes(rows, K)
     if codes is None:
-        codes = like.new_empty(c, dtype=torch.uint8)
+        codes = _empty(c, torch.uint8, like.device, stream)
     if scales is None:
-        scales = like.new_empty(s, dtype=torch.uint8)
+        scales = _empty(s, torch.uint8, like.device, stream)
     return codes, scales
 
 
@@ -751,7 +761,7 @@ def molora_mx_quantize(x, codes=None, scales=None, stream=None):
     rows, K = _two(x, "x")
     if x.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"x must be bfloat16 or float32, got {x.dtype}")
-    codes, scales = _mx_outputs(rows, K, codes, scales, x)
+    codes, scales = _mx_outputs(rows, K, codes, scales, x, stream)
     _call_here("molora_mx_quantize", _dev(x, x.dtype, "x"), int(x.dtype is torch.float32), *_mx(codes, scales, rows, K, "x"), rows, K,
                _stream(stream))
     return codes, scales
@@ -760,7 +770,7 @@ def molora_mx_quantize(x, codes=None, scales=None, stream=None):
 def molora_mx_quantize_w(W, codes=None, scales=None, stream=None):
     """A base weight W [d_in][d_out] (bf16) to 4-bit blocks along d_in: (codes, scales), done once."""
     d_in, d_out = _two(W, "W")
-    codes, scales = _mx_outputs(d_out, d_in, codes, scales, W)
+    codes, scales = _mx_outputs(d_out, d_in, codes, scales, W, stream)
     _call_here("molora_mx_quantize_w", _dev(W, torch.bfloat16, "W"), *_mx(codes, scales, d_out, d_in, "W"), d_in, d_out, _stream(stream))
     return codes, scales
 
@@ -770,7 +780,7 @@ def molora_mx_dequantize(codes, scales, rows, K, out=None, stream=None):
     rows, K = int(rows), int(K)
     args = _mx(codes, scales, rows, K, "operand")
     if out is None:
-        out = codes.new_empty((rows, K), dtype=torch.float32)
+        out = _empty((rows, K), torch.float32, codes.device, stream)
     _call_here("molora_mx_dequantize", *args, _dev(out, torch.float32, "out", (rows, K)), rows, K, _stream(stream))
     return out
 
@@ -780,21 +790,15 @@ def molora_mx_matmul(xc, xs, wc, ws, N, d_in, d_out, h=None, stream=None):
     N, d_in, d_out = int(N), int(d_in), int(d_out)
     args = (*_mx(xc, xs, N, d_in, "x"), *_mx(wc, ws, d_out, d_in, "W"))
     if h is None:
-        h = xc.new_empty((N, d_out), dtype=torch.float32)
+        h = _empty((N, d_out), torch.float32, xc.device, stream)
     _call_here("molora_mx_matmul", *args, _dev(h, torch.float32, "h", (N, d_out)), N, d_in, d_out, _stream(stream))
     return h
 
 
 def _workspace(fn, sizes, workspace, device, stream):
-    """The caller's workspace, or one for this call: from the memory of the stream that the call runs on, so that
-    what is given back at its end is not handed to another stream while the kernels still use it."""
+    """The caller's workspace, or one for this call."""
     if workspace is None:
-        nbytes = max(int(getattr(_lib or load(), fn)(*sizes)), 256)
-        if stream is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        else:
-            with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        workspace = _empty(max(int(getattr(_lib or load(), fn)(*sizes)), 256), torch.uint8, device, stream)
     return _flat_bytes(workspace, "workspace")
 
 
@@ -804,7 +808,7 @@ def molora_apply_mx(x, wc, ws, A, B, r, h=None, workspace=None, stream=None):
     C, _, rank = _three(A, "A")
     d_out = _three(B, "B")[2]
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     bf = torch.bfloat16
     work, work_bytes = _workspace("molora_apply_mx_workspace_bytes", (N, d_in, d_out, C, rank), workspace, x.device, stream)
     _call_here("molora_apply_mx", _dev(x, bf, "x"), *_mx(wc, ws, d_out, d_in, "W"), _dev(A, bf, "A", (C, d_in, rank)),
@@ -841,7 +845,7 @@ def molora_apply_gated(x, W, A=None, B=None, r=None, act="silu", z=None, pre=Non
     ops, sizes, code = _gated_args(x, W, A, B, r, act)
     N, F = sizes[0], sizes[2]
     if z is None:
-        z = torch.empty((N, F), dtype=torch.bfloat16, device=x.device)
+        z = _empty((N, F), torch.bfloat16, x.device, stream)
     work, work_bytes = _workspace("molora_apply_gated_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_apply_gated", *ops, _dev(z, torch.bfloat16, "z", (N, F)), _opt(pre, torch.float32, "pre", (N, 2 * F)), *sizes, code,
                work, work_bytes, _stream(stream))
@@ -866,7 +870,7 @@ def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A
             out.append((None, None))
             continue
         if t is None:
-            t = torch.empty(shape, dtype=bf, device=x.device)
+            t = _empty(shape, bf, x.device, stream)
         out.append((t, _dev(t, bf, f"d{name}", shape)))
     work, work_bytes = _workspace("molora_gated_backward_workspace_bytes", sizes, workspace, x.device, stream)
     _call_here("molora_gated_backward", _dev(dz, bf, "dz", (N, F)), *ops, _dev(pre, torch.float32, "pre", (N, 2 * F)), *(d for _, d in out),
