@@ -737,9 +737,18 @@ def _empty(shape, dtype, device, stream):
     torch.cuda.stream(stream)): a block of the current stream may still be in use by kernels there that nothing
     orders before this call's, and given back early it would go to kernels that nothing orders behind them."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
-        return torch.empty(shape, dtype=dtype, device=device)
+        t = torch.empty(shape, dtype=dtype, device=device)
+    else:
+        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+            t = torch.empty(shape, dtype=dtype, device=device)
+    if _recording:   # what a recorded call writes to belongs to its graph: every replay writes there
+        graph = _recording.get(_stream_now(stream))
+        if graph is not None:
+            graph._memory.append(t)
+    return t
+
+
+_recording = {}   # stream handle -> the Graph that records it
 
 
 def _mx_outputs(rows, K, codes, scales, like, stream):
@@ -885,11 +894,15 @@ class Graph:
         with g.capture():
             molora_route(..., stream=stream); molora_bucket(..., stream=stream); ...
         g.launch()                   # replays on `stream`
+
+    The calls of the feed-forward block may allocate outputs and workspaces while they are recorded: the graph keeps
+    that memory until it is destroyed.  The other calls want theirs from the caller, who keeps it.
     """
 
     def __init__(self, stream):
         self.stream = stream
         self._handle = None
+        self._memory = []
 
     def capture(self):
         graph = self
@@ -897,9 +910,11 @@ class Graph:
         class _Capture:
             def __enter__(self):
                 _check(load().molora_graph_begin(_stream_now(graph.stream)), "molora_graph_begin")
+                _recording[_stream_now(graph.stream)] = graph
 
             def __exit__(self, et, ev, tb):
                 h = ctypes.c_void_p()
+                _recording.pop(_stream_now(graph.stream), None)
                 st = load().molora_graph_end(_stream_now(graph.stream), ctypes.byref(h))
                 if et is None:
                     _check(st, "molora_graph_end")
@@ -920,6 +935,7 @@ class Graph:
         if self._handle is not None:
             load().molora_graph_destroy(self._handle)
             self._handle = None
+            self._memory = []
 
 
 class LaunchTimer:

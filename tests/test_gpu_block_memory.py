@@ -1,5 +1,5 @@
 """Memory that the feed-forward block's calls allocate by themselves: outputs and workspaces on a stream other than the
-current one."""
+current one, and of calls that a graph records."""
 import numpy as np
 import pytest
 
@@ -60,3 +60,38 @@ def test_outputs_are_not_memory_that_the_current_stream_still_uses(block, name, 
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", ["mx_quantize", "mx_matmul", "apply_mx", "apply_gated", "gated_backward"])
+def test_memory_of_a_recorded_call_belongs_to_the_graph(block, name):
+    """A call recorded without outputs and workspace: what it writes on every replay is handed to nobody else,
+    whether or not the caller has kept its outputs."""
+    import torch
+    from paper_2603_15965_amd import binding as mb
+    call = block[name]
+    want = call(None)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    call(side)   # the side stream has the memory, given back
+    side.synchronize()
+    print(f"{name} recorded", flush=True)
+    g, kept = mb.Graph(side), mb.Graph(side)
+    with g.capture():
+        call(side)
+    with kept.capture():
+        got = call(side)
+    with torch.cuda.stream(side):   # all that is free on the stream, of any size that the call can have asked for
+        fresh = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in (1 << 12, 1 << 15, 1 << 18, 1 << 20, 5 << 20) for _ in range(3)]
+    for replay in range(3):
+        for t in got:
+            t.fill_(99)
+        torch.cuda.synchronize()
+        g.launch()
+        kept.launch()
+        side.synchronize()
+        assert all(bool((t == 7).all()) for t in fresh), f"replay {replay} wrote to memory that is another tensor's"
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), f"replay {replay}"
+    g.destroy()
+    kept.destroy()
