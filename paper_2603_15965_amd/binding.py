@@ -868,7 +868,8 @@ def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A
     ops, sizes, code = _gated_args(x, W, A, B, r, act)
     N, d_in, F, C, rank = sizes
     bf = torch.bfloat16
-    unknown = set(need) - {"x", "W", "A", "B"}
+    need = set(need)   # (any iterable, read once)
+    unknown = need - {"x", "W", "A", "B"}
     if unknown:
         raise ValueError(f"need names x, W, A, B: got {', '.join(sorted(map(str, unknown)))}")
     out = []

@@ -1,0 +1,22 @@
+"""Arguments of the feed-forward block's calls that the binding has to look at more closely, without a GPU."""
+import pytest
+import torch
+
+from paper_2603_15965_amd import binding as mb
+
+bf, f32, i32, u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+def t(*shape, dtype=bf):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def test_need_may_be_any_iterable():
+    """A generator is read once: dx is needed, so its buffer is taken (and then found to be on the host)."""
+    x, W, A, B, r = t(16, 64), t(64, 32), t(2, 64, 8), t(2, 8, 32), t(16, dtype=i32)
+    pre, dz = t(16, 32, dtype=f32), t(16, 16)
+    for need in (("x",), ["x"], "x", iter(["x"]), (c for c in "x"), {"x": 1}):
+        with pytest.raises(TypeError, match="device tensor"):
+            mb.molora_gated_backward(dz, x, W, A, B, r, pre, need=need, dx=t(16, 64))
+    with pytest.raises(ValueError, match="dx is given but not needed"):
+        mb.molora_gated_backward(dz, x, W, A, B, r, pre, need=iter(["W"]), dx=t(16, 64))
