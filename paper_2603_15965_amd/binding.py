@@ -726,8 +726,8 @@ def _call_here(fn, *args):
 @functools.lru_cache(maxsize=512)
 def _mx_shapes(rows, K):
     """Shapes of the codes and scales of a microscaled operand."""
-    if rows < 0 or K < 8 or K % 8 != 0:
-        raise ValueError(f"a microscaled operand has K >= 8, a multiple of 8: got {rows} rows of {K}")
+    if rows < 0 or K < 8 or K % 8 != 0 or max(rows, K) >> 31:   # (the library's sizes are of 32 bits)
+        raise ValueError(f"a microscaled operand has K >= 8, a multiple of 8, and less than 2^31 either way: got {rows} rows of {K}")
     tiles = -(-rows // 16)
     return (tiles, -(-K // 128), 64, 16), (tiles, -(-K // 512), 64, 4)
 
@@ -835,6 +835,8 @@ def _gated_args(x, W, A, B, r, act):
     wide = _two(W, "W")[1]
     if wide % 2 != 0:
         raise ValueError(f"W holds a gate and an up half of the same width, not {wide} columns")
+    if max(d_in, wide) >> 31:   # (the library's sizes are of 32 bits)
+        raise ValueError(f"W is less than 2^31 either way, not {d_in} x {wide}")
     if act not in _ACTS:
         raise ValueError(f"act must be one of {', '.join(_ACTS)}, got {act!r}")
     given = [t is not None for t in (A, B, r)]

@@ -20,3 +20,17 @@ def test_need_may_be_any_iterable():
             mb.molora_gated_backward(dz, x, W, A, B, r, pre, need=need, dx=t(16, 64))
     with pytest.raises(ValueError, match="dx is given but not needed"):
         mb.molora_gated_backward(dz, x, W, A, B, r, pre, need=iter(["W"]), dx=t(16, 64))
+
+
+@pytest.mark.parametrize("more", [8, 64])
+def test_sizes_that_do_not_fit_32_bits_are_refused(more):
+    """2^32 + 8 columns are not 8: what the library would be told is looked at before anything is allocated."""
+    wide = (1 << 32) + more
+    with pytest.raises(ValueError, match="2\\^31"):
+        mb.molora_mx_quantize(torch.empty(1, wide, dtype=bf, device="meta"))
+    with pytest.raises(ValueError, match="2\\^31"):
+        mb.molora_mx_quantize_w(torch.empty(8, wide, dtype=bf, device="meta"))
+    with pytest.raises(ValueError, match="2\\^31"):
+        mb.molora_mx_dequantize(t(1, 1, 64, 16, dtype=u8), t(1, 1, 64, 4, dtype=u8), 1, wide)
+    with pytest.raises(ValueError, match="2\\^31"):
+        mb.molora_apply_gated(t(1, 8), torch.empty(8, 2 * wide, dtype=bf, device="meta"))
