@@ -497,7 +497,8 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * dA [C][d_in][rank], dB [C][rank][2 F] DEVICE bf16, each written whole, rounded once from fp32
  * sums; a NULL one is not computed (dA and dB have to be NULL without adapters).  dh is rounded to
  * bf16 before these products.  workspace as above, of
- * molora_gated_backward_workspace_bytes(...) bytes, which never decrease with N.
+ * molora_gated_backward_workspace_bytes(...) bytes, which never decrease with N.  MOLORA_EINVAL (and 0 bytes) also where
+ * C (d_in + 2 F) (rank / 64, rounded up) comes near 2^30: 17 GB of adapters and more.
  *
  * Infinities and NaN in the A or B of an adapter reach the rows of z, pre and dx of its tokens and its own dA and
  * dB, nothing else; workgroups that meet them take twice the time.

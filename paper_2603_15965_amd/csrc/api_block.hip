@@ -111,6 +111,10 @@ inline GatedWorkspace carve_gated(void *base, int64_t N, int32_t d_in, int32_t F
     w.bytes = c.at;
     return w;
 }
+inline int64_t padded_rows(int64_t N) { return (N + 7) & ~int64_t(7); }
+inline bool backward_sizes_ok(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t act) {
+    return gated_sizes_ok(N, d_in, F, C, rank, act) && molora::gated_backward_sizes_ok(N, padded_rows(N), d_in, F, C, rank);
+}
 // Room for any batch of up to N tokens: one of a few tokens may be cut into more slices than one of 64.
 inline size_t gated_workspace_up_to(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
     size_t most = carve_gated(nullptr, N, d_in, F, C, rank).bytes;
@@ -128,7 +132,6 @@ struct BackwardWorkspace {
     size_t outer_a;  // floats of planes that dA takes
     size_t bytes;
 };
-inline int64_t padded_rows(int64_t N) { return (N + 7) & ~int64_t(7); }
 inline BackwardWorkspace carve_backward(void *base, int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
     Cutter c{static_cast<unsigned char *>(base)};
     BackwardWorkspace w{};
@@ -291,14 +294,14 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
 }
 
 size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {
-    return gated_sizes_ok(N, d_in, F, C, rank, 0) ? carve_backward(nullptr, N, d_in, F, C, rank).bytes : 0;
+    return backward_sizes_ok(N, d_in, F, C, rank, 0) ? carve_backward(nullptr, N, d_in, F, C, rank).bytes : 0;
 }
 
 molora_status molora_gated_backward(const void *dz, const void *x, const void *W, const void *A, const void *B,
                                     const int32_t *r, const float *pre, void *dx, void *dW, void *dA, void *dB, int64_t N,
                                     int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t act, void *workspace,
                                     size_t workspace_bytes, void *stream) {
-    if (!gated_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
+    if (!backward_sizes_ok(N, d_in, F, C, rank, act)) return MOLORA_EINVAL;
     if (C == 0 && (dA || dB)) return MOLORA_EINVAL;
     if (N == 0) {  // sums over no tokens
         if (!aligned16(dW) || !aligned16(dA) || !aligned16(dB)) return MOLORA_EALIGN;

@@ -253,6 +253,7 @@ struct GroupedOuter {
     bool flat;
 };
 size_t grouped_outer_floats(int64_t N, int D, int R);
+bool gated_backward_sizes_ok(int64_t N, int64_t padded, int d_in, int F, int C, int R);  // the launches here fit their grids
 hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t *offsets, const int32_t *perm, int64_t N, int C,
                                  int R, hipStream_t s);
 // out [n] bf16 = the sum of `count` planes of n floats (a multiple of 8)

@@ -318,11 +318,21 @@ __global__ __launch_bounds__(256) void sum_pieces_kernel(OuterJobs jobs, const i
 
 // workgroups of a piece
 int64_t outer_tiles(int D, int R) { return (int64_t)((D + kOuterCols - 1) / kOuterCols) * ((R + kOuterR - 1) / kOuterR); }
+// columns of Y to a workgroup, in tiles: where the buckets are short on average and the columns many, one for each wavefront
+bool outer_wide(int64_t N, int D, int C, int R) { return N <= (int64_t)C * kWideRows && outer_tiles(D, R) * C > 1024; }
 // rows of a piece: so many that two workgroups to a compute unit share all rows, and eight steps at least
 int outer_rows(int64_t N, int D, int R) {
     const int64_t rows = (N * outer_tiles(D, R) + 511) / 512;
     return (int)(rows <= kOuterRows ? kOuterRows : (rows + 127) / 128 * 128);
 }
+// workgroups of an outer product, of the sums behind it, and of matrices transposed
+int64_t outer_blocks(int64_t N, int D, int C, int R) {
+    const int64_t tiles = outer_wide(N, D, C, R) ? ((D + kOuterCols - 1) / kOuterCols + 3) / 4 : (D + kOuterCols - 1) / kOuterCols;
+    return tiles * ((R + kOuterR - 1) / kOuterR) * (C + N / outer_rows(N, D, R));
+}
+int64_t sum_blocks(int64_t N, int D, int R) { return ((int64_t)D * R + 2047) / 2048 * (N / outer_rows(N, D, R)); }
+int64_t transpose_blocks(int64_t batch, int64_t cols, int64_t padded) { return batch * ((cols + 63) / 64) * ((padded + 63) / 64); }
+constexpr int64_t kMaxBlocks = int64_t(1) << 24;  // of 256 threads: the runtime counts a launch's threads in 32 bits
 
 }  // namespace
 
@@ -335,7 +345,7 @@ hipError_t launch_zero(void *dst, int64_t bytes, hipStream_t s) {
 
 hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, int64_t N, int F, int act, hipStream_t s) {
     const int64_t items = N * (F / 4), blocks = (items + 255) / 256;
-    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+    if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
     if (blocks > 0) hipLaunchKernelGGL(gate_kernel, dim3((unsigned)blocks), dim3(256), 0, s, planes, count, z, pre, items, F, act);
     return hipGetLastError();
 }
@@ -349,15 +359,21 @@ hipError_t launch_gate_backward(const uint16_t *dz, const float *pre, uint16_t *
         all.first[i] = (int)blocks;
         if (i >= n) continue;
         all.job[i] = jobs[i];
-        blocks += jobs[i].batch * ((jobs[i].cols + 63) / 64) * ((jobs[i].padded + 63) / 64);
-        if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+        blocks += transpose_blocks(jobs[i].batch, jobs[i].cols, jobs[i].padded);
+        if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
     }
     all.first[kMaxTransposes] = (int)blocks;
     const GateBackward gate{dz, pre, dh, N, padded * (F / 4), F, act};
     blocks += (gate.items + 255) / 256;
-    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+    if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
     hipLaunchKernelGGL(gate_backward_kernel, dim3((unsigned)blocks), dim3(256), 0, s, gate, all);
     return hipGetLastError();
+}
+
+bool gated_backward_sizes_ok(int64_t N, int64_t padded, int d_in, int F, int C, int R) {
+    const int64_t turned = transpose_blocks(C, 2 * (int64_t)F, R) + transpose_blocks(C, R, d_in) + transpose_blocks(1, d_in, padded);
+    if (turned + (padded * (F / 4) + 255) / 256 >= kMaxBlocks) return false;
+    return C == 0 || (outer_blocks(N, d_in, C, R) + outer_blocks(N, 2 * F, C, R) < kMaxBlocks && sum_blocks(N, d_in, R) + sum_blocks(N, 2 * F, R) < kMaxBlocks);
 }
 
 size_t grouped_outer_floats(int64_t N, int D, int R) {  // (never less for more rows: what outer_rows gives at most)
@@ -366,7 +382,7 @@ size_t grouped_outer_floats(int64_t N, int D, int R) {  // (never less for more 
 
 hipError_t launch_sum_planes(const float *planes, uint16_t *out, int64_t n, int count, hipStream_t s) {
     const int64_t blocks = (n + 2047) / 2048;
-    if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+    if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
     hipLaunchKernelGGL(sum_planes_kernel, dim3((unsigned)blocks), dim3(256), 0, s, planes, out, n, count);
     return hipGetLastError();
 }
@@ -379,14 +395,14 @@ hipError_t launch_grouped_outers(const GroupedOuter *want, int n, const int32_t 
     for (int i = 0; i < n; ++i) {
         OuterJob &m = jobs.job[i];
         const int rows = outer_rows(N, want[i].D, R), extra = (int)(N / rows);
-        const int tiles = (want[i].D + kOuterCols - 1) / kOuterCols, parts = (R + kOuterR - 1) / kOuterR;
-        const bool wide = N <= (int64_t)C * kWideRows && (int64_t)tiles * parts * C > 1024;
+        const int tiles = (want[i].D + kOuterCols - 1) / kOuterCols;
+        const bool wide = outer_wide(N, want[i].D, C, R);
         m = OuterJob{want[i].y, want[i].s2, want[i].out, want[i].planes, want[i].D, want[i].flat ? 1 : 0,
                      wide ? (tiles + 3) / 4 : tiles, rows, extra, wide ? 1 : 0};
-        blocks += (int64_t)m.tiles * parts * (C + extra);
-        sums += ((int64_t)m.D * R + 2047) / 2048 * extra;
+        blocks += outer_blocks(N, m.D, C, R);
+        sums += sum_blocks(N, m.D, R);
         if (i == 0) jobs.first = (int)blocks, jobs.first_sum = (int)sums;
-        if (blocks >= (int64_t(1) << 24) || sums >= (int64_t(1) << 24)) return hipErrorInvalidValue;
+        if (blocks >= kMaxBlocks || sums >= kMaxBlocks) return hipErrorInvalidValue;
     }
     hipLaunchKernelGGL(grouped_outer_kernel, dim3((unsigned)blocks), dim3(256), 0, s, jobs, offsets, perm, C, R);
     const hipError_t e = hipGetLastError();

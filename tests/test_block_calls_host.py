@@ -34,3 +34,21 @@ def test_sizes_that_do_not_fit_32_bits_are_refused(more):
         mb.molora_mx_dequantize(t(1, 1, 64, 16, dtype=u8), t(1, 1, 64, 4, dtype=u8), 1, wide)
     with pytest.raises(ValueError, match="2\\^31"):
         mb.molora_apply_gated(t(1, 8), torch.empty(8, 2 * wide, dtype=bf, device="meta"))
+
+
+def test_gradients_of_adapters_beyond_a_launch_are_refused_at_once():
+    """Sizes whose last launches do not fit a grid: refused with the others, not when the first ones are on their way."""
+    import ctypes
+    lib = mb.load()
+    buf = (ctypes.c_char * 512)()
+    a = ctypes.addressof(buf)
+    a += -a % 256
+
+    def call(N, d_in, F, C, rank):
+        ws = lib.molora_gated_backward_workspace_bytes(N, d_in, F, C, rank)
+        return ws, lib.molora_gated_backward(a, a, a, a, a, a, a, a, a, a, a, N, d_in, F, C, rank, 0, a, 1 << 40, None)
+    for sizes in ((2000, 8, 1 << 19, 1024, 8), (500, 8, 1 << 21, 1024, 8), (16, 1 << 20, 1016, 1024, 16)):
+        assert call(*sizes) == (0, -1), sizes
+    assert lib.molora_gated_backward_workspace_bytes(2000, 8, 1 << 18, 1024, 8) > 0
+    assert lib.molora_gated_backward_workspace_bytes(8000, 8, 1 << 16, 1024, 128) > 0
+    assert lib.molora_apply_gated_workspace_bytes(2000, 8, 1 << 19, 1024, 8) > 0   # the forward pass has no such launch
