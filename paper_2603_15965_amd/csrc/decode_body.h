@@ -169,12 +169,15 @@ struct BatchAdapters {
 };
 
 // t of NR * 16 rows, the slices added, as bf16 halves [hi | lo] to LDS; zeros where there is no adapter.  512 threads.
+// (Two halves, as in the larger batches: the product takes bf16 operands, and what a third half would hold is 2^-16 of
+// t at most; h of 64 x 4096 -> 12288 is 6e-7 of its norm off, 8e-8 with t in fp32.)
 inline __host__ __device__ constexpr int t_row_bytes(int R) { return 4 * R + 16; }  // (+16: bank shift)
 template <int NR>
-__device__ __forceinline__ void t_to_lds(const float *__restrict__ planes, int slices, int target, int N, int R, unsigned char *t_lds) {
+__device__ __forceinline__ void t_to_lds(const float *__restrict__ planes, int slices, int target, int R, unsigned char *t_lds) {
     constexpr int ITEMS = (NR * 16 * (MOLORA_MAX_RANK / 8) + 511) / 512;  // eight columns of a row
     const int tid = threadIdx.x, lane = tid & 63;
     const int per_row = R / 8, items = NR * 16 * per_row;
+    const uint64_t routed = __ballot(target >= 0);  // the tokens with an adapter (asked of all lanes: a lane that is off has no answer)
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
         const int it = min(tid + u * 512, items - 1), row = it / per_row, col = it % per_row * 8;
@@ -189,7 +192,7 @@ __device__ __forceinline__ void t_to_lds(const float *__restrict__ planes, int s
                 v[1] += v1;
             }
         }
-        const bool own = row < N && __shfl(target, row & 63) >= 0;
+        const bool own = routed >> row & 1;
         u32x4 hi, lo;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {

@@ -124,7 +124,7 @@ __device__ __forceinline__ bool mx_decode_body(const uint8_t *__restrict__ xc, c
         if (kg < kg_n) load(kg);
         batch.find(target, lane);
         if (batch.n > 0) load_slabs(wave);
-        t_to_lds<NR>(planes, slices, target, N, R, t_lds);
+        t_to_lds<NR>(planes, slices, target, R, t_lds);
         while (kg < kg_n) {
             multiply(kg);
             kg += 8;
