@@ -218,6 +218,8 @@ hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t
 struct GemmSlices {
     int slices, config;  // config -1: the streaming kernel
 };
+// The tallest tiles that K goes in slices for (192 rows; of four million random sizes 21 would take 256 rows)
+constexpr int kMaxSlicedConfig = 4;
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming);
 // h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr; planes as above
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,

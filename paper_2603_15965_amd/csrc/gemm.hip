@@ -130,7 +130,7 @@ GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool
     }
     for (int slices = 2; slices <= kMaxGemmSlices; ++slices) {
         if (slices * floats > (double)kMaxPlaneFloats || d_in < slices * 256) break;
-        for (int i = 0; i < kGemmConfigs; ++i) {
+        for (int i = 0; i <= kMaxSlicedConfig; ++i) {
             const double cost = tiled_cost(kGemmCosts[i], N, d_in, d_out, C, R, slices) + second(slices);
             if (cost < best) {
                 best = cost;

@@ -26,29 +26,26 @@ hipError_t launch_config(int config, const uint16_t *x, const uint16_t *W, const
                          const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in, int d_out, int C, int rank,
                          GemmEpilogue ep, int slices, hipStream_t s) {
 #define MOLORA_OUT_ARGS x, W, B, t2, offsets, perm, h, N, d_in, d_out, C, rank, ep, slices, s
+    if constexpr (OUT != kOutPlanes) {  // (kMaxSlicedConfig)
+        if (config == 5) return launch_out<GemmBig, OUT, WT>(MOLORA_OUT_ARGS);
+        if (config == 6) return launch_out<Gemm320, OUT, WT>(MOLORA_OUT_ARGS);
+    }
     switch (config) {  // the order of kGemmCosts
         case 0: return launch_out<Gemm64, OUT, WT>(MOLORA_OUT_ARGS);
         case 1: return launch_out<GemmMid, OUT, WT>(MOLORA_OUT_ARGS);
         case 2: return launch_out<GemmSmall, OUT, WT>(MOLORA_OUT_ARGS);
         case 3: return launch_out<GemmWide, OUT, WT>(MOLORA_OUT_ARGS);
         case 4: return launch_out<Gemm192, OUT, WT>(MOLORA_OUT_ARGS);
-        case 5: return launch_out<GemmBig, OUT, WT>(MOLORA_OUT_ARGS);
-        default: return launch_out<Gemm320, OUT, WT>(MOLORA_OUT_ARGS);
+        default: return hipErrorInvalidValue;
     }
 #undef MOLORA_OUT_ARGS
 }
 
-// fp32 sums of x W + t B_c over slices of K to planes, `count` of them
-template <bool WT>
-hipError_t launch_planes(const GemmSlices &pick, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
-                         const int32_t *offsets, const int32_t *perm, float *planes, int64_t N, int d_in, int d_out, int C,
-                         int rank, int &count, hipStream_t s) {
-    const int k_slice = ((d_in + pick.slices - 1) / pick.slices + 63) / 64 * 64;
-    count = (d_in + k_slice - 1) / k_slice;
-    return launch_config<kOutPlanes, WT>(pick.config, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank,
-                                         GemmEpilogue{nullptr, 0, k_slice}, count, s);
-}
-
 }  // namespace
+
+// fp32 sums of x W + t B_c over slices of K to planes, `count` of them (gemm_planes.hip)
+hipError_t launch_gemm_planes(const GemmSlices &pick, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
+                              const int32_t *offsets, const int32_t *perm, float *planes, int64_t N, int d_in, int d_out, int C,
+                              int rank, bool wt, int &count, hipStream_t s);
 
 }  // namespace molora

@@ -1,5 +1,5 @@
-// The fused GEMM with outputs other than fp32 h: the gated block's z, and fp32 sums of slices of K that a second
-// launch ends in z.  (gemm_grad.hip: bf16 gradients.)
+// The fused GEMM that ends in the gated block's z; where K goes in slices, or the streaming kernel is the cheaper one, fp32 sums
+// and a second launch that ends them.  (gemm_planes.hip: the slices.  gemm_grad.hip: bf16 gradients.)
 //
 // 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16: 346 us (1.19 PFLOP/s, by power) where h is not wanted, 455 with its 403
 // MB, whose stores meet no products: every compute unit holds one workgroup.  In two workgroups of 128 x 128 each the
@@ -20,7 +20,7 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
     const hipError_t e =
         pick.config < 0
             ? launch_small_batch_gemm_own_rows(x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, s)
-            : launch_planes<false>(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, count, s);
+            : launch_gemm_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, false, count, s);
     return e != hipSuccess ? e : launch_gate(planes, count, z, pre, N, F, act, s);
 }
 
