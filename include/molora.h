@@ -545,7 +545,8 @@ void molora_graph_destroy(molora_graph *graph);
  * hands it to the calling thread's next launch of such a kernel -- the tiled GEMM of
  * molora_base_expand* / molora_apply*, the small-batch GEMM of the same calls, the one launch that
  * molora_apply of a small batch with a few narrow adapters is, the launch of
- * molora_shrink_base_small* -- which records its start and end on it; other launches pass it
+ * molora_shrink_base_small*, the product of molora_mx_matmul and molora_apply_mx, the launch of
+ * molora_apply_gated that reads W -- which records its start and end on it; other launches pass it
  * by, a timer armed later replaces it, and a launch under stream capture must not be given one.
  * molora_launch_timer_elapsed_us waits for that launch to finish (the only call of the
  * library that blocks) and returns its duration; MOLORA_EHIP if no launch took the timer, also of one

@@ -15,7 +15,7 @@ hipError_t launch_gemm_bf16(const uint16_t *x, const uint16_t *W, const uint16_t
         return wt ? launch_config<kOutBf16, true>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, ep, 1, s)
                   : launch_config<kOutBf16, false>(pick.config, x, W, B, t2, offsets, perm, nullptr, N, d_in, d_out, C, rank, ep, 1, s);
     int count;
-    const hipError_t e = launch_gemm_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, wt, count, s);
+    const hipError_t e = launch_gemm_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, d_out, C, rank, wt, false, count, s);
     return e != hipSuccess ? e : launch_sum_planes(planes, out, N * d_out, count, s);
 }
 

@@ -104,6 +104,7 @@ struct GemmEpilogue {
     uint16_t *out16 = nullptr;  // bf16 h, or z
     int act = 0;                // kOutGated: the activation
     int k_slice = 0;            // kOutPlanes: k of a slice, a multiple of 64
+    bool base = false;          // a base projection's launch, which takes the launch timer (a gradient's does not)
 };
 
 // (two wavefronts per SIMD at least: with 512 registers to a wavefront the compiler keeps the accumulators in

@@ -16,8 +16,12 @@ hipError_t launch_out(const uint16_t *x, const uint16_t *W, const uint16_t *B, c
     const int tiles_n = (cols + per - 1) / per;
     const unsigned blocks = (unsigned)(((int64_t)tiles_m * tiles_n + 7) / 8 * 8);
     constexpr auto kernel = fused_gemm_kernel<Cfg, OUT, WT>;
-    hipLaunchKernelGGL(kernel, dim3(blocks, (unsigned)slices), dim3(Cfg::NT), Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h,
-                       (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, Mix{1, C, nullptr, nullptr}, ep);
+    const dim3 grid(blocks, (unsigned)slices), block(Cfg::NT);
+    const Mix plain{1, C, nullptr, nullptr};
+    if (ep.base)
+        launch_base_kernel(kernel, grid, block, Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, plain, ep);
+    else
+        hipLaunchKernelGGL(kernel, grid, block, Cfg::LDS_BYTES, s, x, W, B, t2, offsets, perm, h, (int)N, d_in, d_out, C, rank, tiles_m, tiles_n, plain, ep);
     return hipGetLastError();
 }
 
@@ -46,6 +50,6 @@ hipError_t launch_config(int config, const uint16_t *x, const uint16_t *W, const
 // fp32 sums of x W + t B_c over slices of K to planes, `count` of them (gemm_planes.hip)
 hipError_t launch_gemm_planes(const GemmSlices &pick, const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                               const int32_t *offsets, const int32_t *perm, float *planes, int64_t N, int d_in, int d_out, int C,
-                              int rank, bool wt, int &count, hipStream_t s);
+                              int rank, bool wt, bool base, int &count, hipStream_t s);
 
 }  // namespace molora

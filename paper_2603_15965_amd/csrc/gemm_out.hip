@@ -15,12 +15,12 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
     const GemmSlices pick = sliced_gemm_choice(N, d_in, 2 * F, C, rank, perm != nullptr);
     if (pick.slices == 1 && pick.config >= 0)
         return launch_config<kOutGated, false>(pick.config, x, W, B, t2, offsets, perm, pre, N, d_in, 2 * F, C, rank,
-                                               GemmEpilogue{z, act}, 1, s);
+                                               GemmEpilogue{z, act, 0, true}, 1, s);
     int count = 1;
     const hipError_t e =
         pick.config < 0
             ? launch_small_batch_gemm_own_rows(x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, s)
-            : launch_gemm_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, false, count, s);
+            : launch_gemm_planes(pick, x, W, B, t2, offsets, perm, planes, N, d_in, 2 * F, C, rank, false, true, count, s);
     return e != hipSuccess ? e : launch_gate(planes, count, z, pre, N, F, act, s);
 }
 

@@ -208,8 +208,7 @@ template <int NR, int CT, class... Args>
 void launch_decode(unsigned blocks, int rank, hipStream_t s, Args... args) {
     (void)&DecodeKernel<NR, CT>::lds;  // instantiates the registration
     constexpr auto kernel = mx_decode_kernel<NR, CT>;
-    const int bytes = DecodeLds<NR, CT>::bytes(rank);
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(512), bytes, s, args...);
+    launch_base_kernel(kernel, dim3(blocks), dim3(512), (size_t)DecodeLds<NR, CT>::bytes(rank), s, args...);
 }
 
 }  // namespace

@@ -375,7 +375,7 @@ hipError_t launch_mx_tiles(const uint8_t *xc, const uint8_t *xs, const uint8_t *
     const int64_t tiles_m = (N + Cfg::BM - 1) / Cfg::BM, tiles_n = (d_out + Cfg::BN - 1) / Cfg::BN;
     const int64_t blocks = (tiles_m * tiles_n + 7) / 8 * 8;
     if (blocks * Cfg::NT >= (int64_t(1) << 32)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(mx_gemm_kernel<Cfg>, dim3((unsigned)blocks), dim3(Cfg::NT), Cfg::LDS_BYTES, s, xc, xs, wc, ws, B, t2,
+    launch_base_kernel(mx_gemm_kernel<Cfg>, dim3((unsigned)blocks), dim3(Cfg::NT), Cfg::LDS_BYTES, s, xc, xs, wc, ws, B, t2,
                        offsets, perm, h, (int)N, d_out, mx_k_tiles(d_in), mx_k_groups(d_in), C, rank, (int)tiles_m, (int)tiles_n);
     return hipGetLastError();
 }
