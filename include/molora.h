@@ -457,6 +457,8 @@ molora_status molora_apply_mix(const void *x, const void *W, const void *A, cons
  *                        What is not finite in a row of x reaches that row of h, what is not in an adapter's A or B
  *                        the rows of its tokens (each takes twice the time where it occurs), no others.
  * All pointers DEVICE, 16-byte aligned (workspace 256).  Errors as molora_apply.
+ * molora_mx_matmul_tile  as molora_base_expand_tile: the tile that the two products take for these sizes, tile[0]
+ *                        rows, tile[1] columns, tile[2] LDS stages, 0 for the kernel of at most 64 tokens.
  */
 size_t molora_mx_codes_bytes(int64_t rows, int32_t K);
 size_t molora_mx_scales_bytes(int64_t rows, int32_t K);
@@ -468,6 +470,7 @@ molora_status molora_mx_dequantize(const void *codes, const void *scales, float 
                                    int32_t K, void *stream);
 molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, const void *ws, float *h,
                                int64_t N, int32_t d_in, int32_t d_out, void *stream);
+molora_status molora_mx_matmul_tile(int64_t N, int32_t d_in, int32_t d_out, int32_t *tile);
 size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank);
 molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, const void *A,
                               const void *B, const int32_t *r, float *h, int64_t N, int32_t d_in,
@@ -502,12 +505,19 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  *
  * Infinities and NaN in the A or B of an adapter reach the rows of z, pre and dx of its tokens and its own dA and
  * dB, nothing else; workgroups that meet them take twice the time.
+ *
+ * molora_apply_gated_tile, molora_gated_backward_tile: as molora_base_expand_tile, of the launch that holds x W and of
+ * the products dx and dW; tile[3] is the number of slices of K.  Of at most 64 tokens: rows and columns (of both
+ * halves) of the second launch's workgroups, 0 stages, and the slices of x W.
  */
 size_t molora_apply_gated_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank);
 molora_status molora_apply_gated(const void *x, const void *W, const void *A, const void *B,
                                  const int32_t *r, void *z, float *pre, int64_t N, int32_t d_in, int32_t F,
                                  int32_t C, int32_t rank, int32_t act, void *workspace,
                                  size_t workspace_bytes, void *stream);
+molora_status molora_apply_gated_tile(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t *tile);
+molora_status molora_gated_backward_tile(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank,
+                                         int32_t *dx_tile, int32_t *dW_tile);
 size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank);
 molora_status molora_gated_backward(const void *dz, const void *x, const void *W, const void *A,
                                     const void *B, const int32_t *r, const float *pre, void *dx, void *dW,

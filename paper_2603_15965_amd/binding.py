@@ -27,7 +27,7 @@ EXPORTS = ["molora_route", "molora_route_vocab", "molora_bucket", "molora_apply_
            "molora_mx_codes_bytes", "molora_mx_scales_bytes", "molora_mx_quantize", "molora_mx_quantize_w",
            "molora_mx_dequantize", "molora_mx_matmul", "molora_apply_mx_workspace_bytes", "molora_apply_mx",
            "molora_apply_gated_workspace_bytes", "molora_apply_gated", "molora_gated_backward_workspace_bytes",
-           "molora_gated_backward",
+           "molora_gated_backward", "molora_mx_matmul_tile", "molora_apply_gated_tile", "molora_gated_backward_tile",
            "molora_graph_begin", "molora_graph_end", "molora_graph_launch", "molora_graph_destroy",
            "molora_launch_timer_create", "molora_launch_timer_arm", "molora_launch_timer_elapsed_us",
            "molora_launch_timer_destroy",
@@ -140,6 +140,11 @@ def load():
     lib.molora_apply_gated.restype = ctypes.c_int
     lib.molora_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
     lib.molora_gated_backward.restype = ctypes.c_int
+    lib.molora_mx_matmul_tile.argtypes = [i64, i32, i32, vp]
+    lib.molora_apply_gated_tile.argtypes = [i64, i32, i32, i32, i32, vp]
+    lib.molora_gated_backward_tile.argtypes = [i64, i32, i32, i32, i32, vp, vp]
+    for f in (lib.molora_mx_matmul_tile, lib.molora_apply_gated_tile, lib.molora_gated_backward_tile):
+        f.restype = ctypes.c_int
     lib.molora_graph_begin.argtypes = [vp]
     lib.molora_graph_begin.restype = ctypes.c_int
     lib.molora_graph_end.argtypes = [vp, ctypes.POINTER(vp)]
@@ -888,6 +893,29 @@ def molora_gated_backward(dz, x, W, A, B, r, pre, act="silu", need=("x", "W", "A
     _call_here("molora_gated_backward", _dev(dz, bf, "dz", (N, F)), *ops, _dev(pre, torch.float32, "pre", (N, 2 * F)), *(d for _, d in out),
                *sizes, code, work, work_bytes, _stream(stream))
     return tuple(t for t, _ in out)
+
+
+def molora_mx_matmul_tile(N, d_in, d_out):
+    """(rows, columns, LDS stages) of the tile that molora_mx_matmul and molora_apply_mx take for these sizes; 0
+    stages: the kernel of at most 64 tokens."""
+    tile = (ctypes.c_int32 * 3)()
+    _check(load().molora_mx_matmul_tile(N, d_in, d_out, tile), "molora_mx_matmul_tile")
+    return tuple(tile)
+
+
+def molora_apply_gated_tile(N, d_in, F, C=0, rank=0):
+    """(rows, columns, LDS stages, slices of K) of molora_apply_gated; 0 stages: the streaming kernel, or at most 64
+    tokens."""
+    tile = (ctypes.c_int32 * 4)()
+    _check(load().molora_apply_gated_tile(N, d_in, F, C, rank, tile), "molora_apply_gated_tile")
+    return tuple(tile)
+
+
+def molora_gated_backward_tile(N, d_in, F, C=0, rank=0):
+    """The same of molora_gated_backward's products: (dx's tile, dW's tile)."""
+    dx, dW = (ctypes.c_int32 * 4)(), (ctypes.c_int32 * 4)()
+    _check(load().molora_gated_backward_tile(N, d_in, F, C, rank, dx, dW), "molora_gated_backward_tile")
+    return tuple(dx), tuple(dW)
 
 
 class Graph:

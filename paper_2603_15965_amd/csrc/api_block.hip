@@ -230,6 +230,12 @@ molora_status molora_mx_matmul(const void *xc, const void *xs, const void *wc, c
                                            static_cast<hipStream_t>(stream)));
 }
 
+molora_status molora_mx_matmul_tile(int64_t N, int32_t d_in, int32_t d_out, int32_t *tile) {
+    if (!tile || N < 1 || !mx_product_ok(N, d_in, d_out)) return MOLORA_EINVAL;
+    molora::mx_gemm_tile(N, d_in, d_out, tile);
+    return MOLORA_OK;
+}
+
 size_t molora_apply_mx_workspace_bytes(int64_t N, int32_t d_in, int32_t d_out, int32_t C, int32_t rank) {
     if (!apply_sizes_ok(N, d_in, d_out, C, rank) || !mx_product_ok(N, d_in, d_out)) return 0;
     const size_t a = carve_mx(nullptr, N, d_in, C, rank).bytes, b = carve_mx(nullptr, N < kDecode ? N : kDecode, d_in, C, rank).bytes;
@@ -291,6 +297,26 @@ molora_status molora_apply_gated(const void *x, const void *W, const void *A, co
     }
     if (C > 0) MOLORA_TRY(dispatch_shrink(r, xb, Ab, w.offsets, w.perm, w.t2, w.planes, N, d_in, C, rank, s));
     return from_hip(molora::launch_gemm_gated(xb, Wb, Bb, w.t2, w.offsets, w.perm, pre, zb, w.planes, N, d_in, F, C, rank, act, s));
+}
+
+molora_status molora_apply_gated_tile(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t *tile) {
+    if (!tile || N < 1 || !gated_sizes_ok(N, d_in, F, C, rank, 0)) return MOLORA_EINVAL;
+    if (N <= kDecode) {
+        tile[0] = (int32_t)(N + 15) / 16 * 16;
+        tile[1] = 2 * molora::gated_finish_cols(F);
+        tile[2] = 0;
+        tile[3] = molora::small_base_slices_rounds(N, d_in, 2 * F, C);
+    } else {
+        molora::sliced_gemm_tile(N, d_in, 2 * F, C, rank, C > 0, tile);
+    }
+    return MOLORA_OK;
+}
+
+molora_status molora_gated_backward_tile(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank, int32_t *dx_tile, int32_t *dW_tile) {
+    if (!dx_tile || !dW_tile || N < 1 || !backward_sizes_ok(N, d_in, F, C, rank, 0)) return MOLORA_EINVAL;
+    molora::sliced_gemm_tile(N, 2 * F, d_in, C, rank, false, dx_tile);
+    molora::sliced_gemm_tile(d_in, (int)padded_rows(N), 2 * F, 0, 0, false, dW_tile);
+    return MOLORA_OK;
 }
 
 size_t molora_gated_backward_workspace_bytes(int64_t N, int32_t d_in, int32_t F, int32_t C, int32_t rank) {

@@ -221,6 +221,8 @@ struct GemmSlices {
 // The tallest tiles that K goes in slices for (192 rows; of four million random sizes 21 would take 256 rows)
 constexpr int kMaxSlicedConfig = 4;
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming);
+inline int gemm_k_slice(int d_in, int slices) { return ((d_in + slices - 1) / slices + 63) / 64 * 64; }  // k of a slice
+void sliced_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, bool streaming, int32_t *tile);  // as fused_gemm_tile, and the slices
 // h = x W + t B_c of d_out = 2 F columns, z [N][F] = act(h[:, :F]) h[:, F:] in bf16; h is stored where pre != nullptr; planes as above
 hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_t *B, const uint16_t *t2,
                              const int32_t *offsets, const int32_t *perm, float *pre, uint16_t *z, float *planes, int64_t N,
@@ -232,6 +234,7 @@ hipError_t launch_gemm_gated(const uint16_t *x, const uint16_t *W, const uint16_
 hipError_t launch_gated_finish(const float *base, const float *planes, int slices, const uint16_t *B, const int32_t *r,
                                const uint16_t *t2, const int32_t *perm, uint16_t *z, float *pre, int64_t N, int F, int C, int rank,
                                int act, hipStream_t s);
+int gated_finish_cols(int F);  // columns of z of a workgroup
 // h = the sum of `count` planes [N][2 F], z from it, h stored where pre != nullptr
 hipError_t launch_gate(const float *planes, int count, uint16_t *z, float *pre, int64_t N, int F, int act, hipStream_t s);
 // dh [padded][2 F] bf16 from dz [N][F] and pre [N][2 F], rows N .. padded - 1 zero; in the same launch, for n jobs,

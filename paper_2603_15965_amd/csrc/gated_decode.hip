@@ -203,13 +203,15 @@ void launch_finish(unsigned blocks, int rank, hipStream_t s, Args... args) {
 
 }  // namespace
 
+// as many columns to a workgroup as leave one for every compute unit: pieces of B's rows are longer (three tiles, one
+// workgroup to each unit at F = 12288, instead of four: 20 us at best and more at the median)
+int gated_finish_cols(int F) { return F <= 4096 ? 16 : F <= 8192 ? 32 : 64; }
+
 hipError_t launch_gated_finish(const float *base, const float *planes, int slices, const uint16_t *B, const int32_t *r,
                                const uint16_t *t2, const int32_t *perm, uint16_t *z, float *pre, int64_t N, int F, int C, int rank,
                                int act, hipStream_t s) {
     if (N < 1 || N > 64) return hipErrorInvalidValue;
-    // as many columns to a workgroup as leave one for every compute unit: pieces of B's rows are longer (three tiles, one
-    // workgroup to each unit at F = 12288, instead of four: 20 us at best and more at the median)
-    const int tiles = (F + 15) / 16, ct = tiles <= 256 ? 1 : tiles <= 512 ? 2 : 4;
+    const int tiles = (F + 15) / 16, ct = gated_finish_cols(F) / 16;
     const unsigned blocks = (unsigned)((tiles + ct - 1) / ct);
 #define MOLORA_FINISH(NR, CT) launch_finish<NR, CT>(blocks, rank, s, base, planes, slices, B, r, t2, perm, z, pre, (int)N, F, C, rank, act)
 #define MOLORA_FINISH_ROWS(NR)                  \

@@ -141,13 +141,23 @@ GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool
     return pick;
 }
 
-void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile) {
+namespace {
+void name_tile(int pick, int64_t N, int d_out, int32_t *tile) {
     static constexpr int stages[kGemmConfigs] = {Gemm64::STAGES,   GemmMid::STAGES, GemmSmall::STAGES, GemmWide::STAGES,
                                                  Gemm192::STAGES, GemmBig::STAGES, Gemm320::STAGES};  // the order of kGemmCosts
-    const int pick = gemm_choice(N, d_in, d_out, C, R);
     tile[0] = pick < 0 ? 64 : kGemmCosts[pick].bm;
     tile[1] = pick < 0 ? small_batch_cols(N, d_out) : kGemmCosts[pick].bn;
     tile[2] = pick < 0 ? 0 : stages[pick];
+}
+}  // namespace
+void fused_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, int32_t *tile) {
+    name_tile(gemm_choice(N, d_in, d_out, C, R), N, d_out, tile);
+}
+void sliced_gemm_tile(int64_t N, int d_in, int d_out, int C, int R, bool streaming, int32_t *tile) {
+    const GemmSlices pick = sliced_gemm_choice(N, d_in, d_out, C, R, streaming);
+    name_tile(pick.config, N, d_out, tile);
+    const int k_slice = gemm_k_slice(d_in, pick.slices);
+    tile[3] = pick.config < 0 ? 1 : (d_in + k_slice - 1) / k_slice;
 }
 
 // force_tile: 0 = the choice below; 64 / 128 / 256 = that row-tile height whatever the shape

@@ -44,4 +44,8 @@ hipError_t launch_mx_decode(const uint8_t *xc, const uint8_t *xs, const uint8_t 
                             const int32_t *r, const float *planes, float *h, int64_t N, int d_in, int d_out, int C, int rank,
                             hipStream_t s);
 
+int mx_decode_cols(int d_out);  // columns of a workgroup of the second
+// the kernel that a product takes: rows, columns and stages of its tiles; 0 stages: at most 64 tokens
+void mx_gemm_tile(int64_t N, int d_in, int d_out, int32_t *tile);
+
 }  // namespace molora

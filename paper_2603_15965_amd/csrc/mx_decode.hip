@@ -223,15 +223,17 @@ hipError_t launch_mx_decode_first(const uint16_t *x, const uint16_t *A, const in
     return hipGetLastError();
 }
 
+// as many columns to a workgroup as leave one for every compute unit: what else would run in its place would
+// read all of x and of t again
+int mx_decode_cols(int d_out) { return d_out <= 4096 ? 16 : d_out <= 8192 ? 32 : 48; }
+
 hipError_t launch_mx_decode(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, const uint8_t *ws, const uint16_t *B,
                             const int32_t *r, const float *planes, float *h, int64_t N, int d_in, int d_out, int C, int rank,
                             hipStream_t s) {
     if (N < 1 || N > 64) return hipErrorInvalidValue;
     const int kt = mx_k_tiles(d_in), kg = mx_k_groups(d_in), slices = C > 0 ? decode_slices(N, d_in, C, rank) : 1;
     const int64_t tiles = ((int64_t)d_out + 15) / 16;
-    // as many columns to a workgroup as leave one for every compute unit: what else would run in its place would
-    // read all of x and of t again
-    const int ct = tiles <= 256 ? 1 : tiles <= 512 ? 2 : 3;
+    const int ct = mx_decode_cols(d_out) / 16;
     const unsigned blocks = (unsigned)((tiles + ct - 1) / ct);
 #define MOLORA_MX_DECODE(NR, CT) launch_decode<NR, CT>(blocks, rank, s, xc, xs, wc, ws, B, r, planes, h, (int)N, d_out, kt, kg, C, rank, slices)
 #define MOLORA_MX_DECODE_ROWS(NR)                    \

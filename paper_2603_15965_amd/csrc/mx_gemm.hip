@@ -423,6 +423,14 @@ int mx_tile_choice(int64_t N, int d_in, int d_out) {
 }
 }  // namespace
 
+void mx_gemm_tile(int64_t N, int d_in, int d_out, int32_t *tile) {
+    static constexpr int stages[] = {Mx256::STAGES, MxWide::STAGES, Mx128::STAGES, Mx128Deep::STAGES, MxLow::STAGES, Mx64::STAGES};  // the order of kMxCosts
+    const int pick = N <= 64 ? -1 : mx_tile_choice(N, d_in, d_out);
+    tile[0] = pick < 0 ? (int)mx_row_tiles(N) * 16 : kMxCosts[pick].bm;
+    tile[1] = pick < 0 ? mx_decode_cols(d_out) : kMxCosts[pick].bn;
+    tile[2] = pick < 0 ? 0 : stages[pick];
+}
+
 hipError_t launch_mx_gemm(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, const uint8_t *ws, const uint16_t *B,
                           const uint16_t *t2, const int32_t *offsets, const int32_t *perm, float *h, int64_t N, int d_in,
                           int d_out, int C, int rank, hipStream_t s) {
