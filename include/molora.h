@@ -488,7 +488,7 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * it, for the backward pass; without, z is made from the sums in the GEMM's registers, and a batch too small
  * to occupy the GPU keeps partial sums in the workspace.
  * Without adapters: A, B, r NULL, C = rank = 0.  act: MOLORA_ACT_*.  F >= 8 and a multiple of 8; x, W
- * and h in bf16 below 4 GiB each.  workspace DEVICE, 256-byte aligned, of
+ * and h in bf16 below 4 GiB each, N counted as N + 7.  workspace DEVICE, 256-byte aligned, of
  * molora_apply_gated_workspace_bytes(...) bytes, which never decrease with N.  Errors as molora_apply.
  *
  * molora_gated_backward: the gradients of a scalar loss whose gradient with respect to z is dz (DEVICE bf16
@@ -582,7 +582,7 @@ molora_status molora_init(void);
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *molora_status_string(molora_status status);
 
-/* Library version string, e.g. "molora-gfx950 1.4" (static storage). */
+/* Library version string, e.g. "molora-gfx950 1.5" (static storage). */
 const char *molora_version(void);
 
 #ifdef __cplusplus

@@ -124,8 +124,8 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward gate, T
 // A bucket of more than `rows` rows is cut into even pieces of their own workgroups, whose fp32 sums go to planes and are
 // added by a second launch in a fixed order.  The launch has a piece for every bucket and then as many more as there
 // can be (N / rows), whichever buckets turn out to be the long ones; `rows` is what the workgroups of a compute unit
-// share evenly.  It is bound by reading dh and x: 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16, level routing, 48 us
-// (235 MB).  16384 x 512 -> 2 x 1024, 48 of rank 128 and one of them for all tokens: 84 us, in whole buckets 129; with
+// share evenly.  It is bound by reading dh and x: 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16, level routing, 41 us
+// (235 MB) and 5 for the sums.  16384 x 512 -> 2 x 1024, 48 of rank 128 and one of them for all tokens: 84 us, in whole buckets 129; with
 // level routing cut buckets cost the second launch, 5 us.
 // Where the buckets are short on average (kWideRows) and the columns many, the wavefronts take 64 columns of Y each instead,
 // all rows and no sum: with one step of rows to a bucket three of four had nothing to do.  168 x 1792 -> 2 x 1536, 59 of

@@ -4,7 +4,7 @@
 //     h = sum of the slices + t B_r,   z = act(h[:, :F]) * h[:, F:]
 //
 // ends in z; h is stored only where it is asked for.  It is bound by reading the B_c in use: 64 x 4096 -> 2 x 12288, 16
-// adapters of rank 64 under skewed routing, 20 us behind the first launch's 58 (201 MB of W, 3.5 TB/s).  Streaming both
+// adapters of rank 64 under skewed routing, 20 us behind the first launch's 59 (201 MB of W, 3.4 TB/s).  Streaming both
 // halves of W in this kernel, without the first launch's slices of K: 84 us in all.
 #include "decode_body.h"
 #include "gate.h"

@@ -116,6 +116,10 @@ int gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming = t
 // output tiles, long K), and a second launch that ends them.  1459 x 9216 -> 2 x 256, gated: 76 us in one launch, 53 in
 // slices; a training step of 381 x 256 -> 2 x 512 with 29 adapters of rank 64 90 / 66 us.  (Sixteen slices at most instead of eight: no
 // difference over thirty random shapes.)
+// The costs are the fits above, of fp32 h.  For these outputs, every tile and two, four and eight slices of K forced on 60
+// random shapes (65 .. 16384 tokens, 256 .. 8192 wide, 1 .. 64 adapters, times of the whole call): the choice is behind the
+// best way by 1.7 % for z, 2.1 % for z with h, 1.3 % for dx and 1.8 % for dW (geometric means; 3 to 7 % of the shapes by
+// more than 10 %: 410 x 7608 -> 2 x 2912 85 us, in two slices 68; dW of 207 x 7168 -> 2 x 5376 92, in 128 x 128 tiles 67).
 GemmSlices sliced_gemm_choice(int64_t N, int d_in, int d_out, int C, int R, bool streaming) {
     GemmSlices pick{1, gemm_choice(N, d_in, d_out, C, R, false)};
     double best = tiled_cost(kGemmCosts[pick.config], N, d_in, d_out, C, R);

@@ -1,5 +1,5 @@
-// The fused GEMM with bf16 outputs: gradients in their parameters' type.  8192 tokens, W 2048 x 12288: dx 311 us, dW 340
-// (1.33 and 1.21 PFLOP/s, by power).
+// The fused GEMM with bf16 outputs: gradients in their parameters' type.  8192 tokens, W 2048 x 12288: dx 289 us, dW 317
+// (1.43 and 1.30 PFLOP/s, by power).
 #include "gemm_out.h"
 
 namespace molora {

@@ -1,9 +1,9 @@
 // The fused GEMM that ends in the gated block's z; where K goes in slices, or the streaming kernel is the cheaper one, fp32 sums
 // and a second launch that ends them.  (gemm_planes.hip: the slices.  gemm_grad.hip: bf16 gradients.)
 //
-// 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16: 346 us (1.19 PFLOP/s, by power) where h is not wanted, 455 with its 403
-// MB, whose stores meet no products: every compute unit holds one workgroup.  In two workgroups of 128 x 128 each the
-// same takes 510 us, in 320 x 256 tiles 452.
+// 8192 x 2048 -> 2 x 6144, 8 adapters of rank 16, launch timer: 329 us (1.25 PFLOP/s, by power) where h is not wanted, 385
+// with its 403 MB, whose stores meet no products: every compute unit holds one workgroup.  Back to back with the rest of a
+// training step it is 430; when it was 455, two workgroups of 128 x 128 each took 510 and 320 x 256 tiles 452.
 #include "gemm_out.h"
 
 namespace molora {

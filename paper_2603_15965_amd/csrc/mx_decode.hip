@@ -5,9 +5,9 @@
 //           of adapters in use alone would leave most of the chip idle
 //   second  h = Q(x) Q(W) + t B_r, the slices of t added on the way
 //
-// 64 x 4096 -> 12288, 16 adapters of rank 64 under skewed routing: 25 us, 7 of the first launch and 19 of the second for
-// 46 MB (27 of codes and scales, 19 of B): three trips to memory one after the other (codes of W and t, then B in two
-// batches) in the one workgroup of a compute unit.  With a sort and the tiled product: 40 us.  The product alone of one
+// 64 x 4096 -> 12288, 16 adapters of rank 64 under skewed routing: 26 us, 7 of the first launch and 19 of the second for
+// 46 MB (27 of codes and scales, 19 of B, whose lines neighbouring workgroups on two XCDs both fetch: 73 are read): three
+// trips to memory one after the other (codes of W and t, then B in two batches) in the one workgroup of a compute unit.  With a sort and the tiled product: 40 us.  The product alone of one
 // token, 4096 -> 4096: 3.5 us, a launch.
 #include <type_traits>
 

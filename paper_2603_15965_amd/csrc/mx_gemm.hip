@@ -22,7 +22,8 @@ namespace {
 // 8192 x 12288 -> 4096: 176 us, 4.7 PFLOP/s.  On random codes the instruction sustains 6.9 from registers and 6.2 with its
 // operands read from LDS at this tile's rate (zeros 9.7 and 8.3: power); without the loads of the loop the kernel takes
 // 161 us.  Reads in front of a k tile's products instead of behind the products before: 204 us; two barriers and
-// stages of 256 k, 258.  With d_in = 4096 the stores of h count: 16384 x 4096 -> 12288 takes 400 us, 805 MB of them.
+// stages of 256 k, 258.  With d_in = 4096 the stores of h count: 16384 x 4096 -> 12288 takes 420 us in steady
+// runs (403 at best; 440 to 490 under a kernel trace), 805 MB of them.
 template <int WM_, int WN_, int TM_, int TN_, int STAGES_>
 struct MxCfg {
     static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, STAGES = STAGES_;
@@ -395,7 +396,8 @@ namespace {
 // grow with its share of the places.  Coefficients: non-negative least squares of the relative error over 128
 // shapes, 65 .. 16384 rows, 256 .. 12288 deep, 1024 .. 12288 wide, every configuration timed on each with its operands
 // from HBM.  The choice is 3 % behind the best configuration there (geometric mean, but for a few timings that were
-// disturbed at most 26 %).
+// disturbed at most 26 %).  Over 60 products of 8 .. 1024 columns, which the fit has not seen, it is 1.3 % behind (at most
+// 21 %: 12586 x 768 -> 488 13.2 us, in 64 x 64 tiles 10.9).
 struct MxCost {
     int bm, bn, per_cu;
     double once, round, part, last, k_round, k_part, k_last;
