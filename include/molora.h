@@ -504,7 +504,8 @@ molora_status molora_apply_mx(const void *x, const void *wc, const void *ws, con
  * C (d_in + 2 F) (rank / 64, rounded up) comes near 2^30: 17 GB of adapters and more.
  *
  * Infinities and NaN in the A or B of an adapter reach the rows of z, pre and dx of its tokens and its own dA and
- * dB, nothing else; workgroups that meet them take twice the time.
+ * dB, nothing else; those in a row of x, pre or dz that row of z, pre and dx, dW, and dA and dB of its adapter.
+ * Workgroups that meet them take twice the time.
  *
  * molora_apply_gated_tile, molora_gated_backward_tile: as molora_base_expand_tile, of the launch that holds x W and of
  * the products dx and dW; tile[3] is the number of slices of K.  Of at most 64 tokens: rows and columns (of both

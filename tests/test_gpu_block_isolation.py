@@ -100,3 +100,32 @@ def test_gradients(N, d_in, F, C, rank):
     for a, b in zip(clean[2:], got[2:]):
         keep = [c for c in range(C) if c != 1]
         assert torch.equal(a[keep], b[keep]) and not bool(torch.isfinite(b[1].float()).all())
+
+
+@pytest.mark.parametrize("N,d_in,F,C,rank", [(2, 72, 72, 2, 8), (33, 264, 40, 3, 16), (64, 136, 4120, 5, 40), (66, 72, 72, 11, 32),
+                                             (300, 264, 520, 4, 24), (515, 520, 264, 7, 16), (2056, 72, 136, 70, 8)])
+def test_rows_that_are_not_finite(N, d_in, F, C, rank):
+    """A row of x, and a value of dz, reach their own row and the gradients that sum over it, no other row or adapter."""
+    print(f"spoiled rows: {N} x {d_in} -> 2 x {F}, {C} of rank {rank}", flush=True)
+    torch, mb, x, W, A, B, r, rd = _case(N, d_in, 2 * F, C, rank)
+    rows = np.zeros(N, bool)
+    rows[[0, N - 1]] = True
+    x2 = x.clone()
+    x2[0, d_in - 1], x2[N - 1, 0] = float("inf"), float("nan")
+    pre, pre2 = (torch.empty(N, 2 * F, dtype=torch.float32, device="cuda") for _ in range(2))
+    z = mb.molora_apply_gated(x, W, A, B, rd, pre=pre)
+    z2 = mb.molora_apply_gated(x2, W, A, B, rd, pre=pre2)
+    _same_but(torch, z, z2, rows)
+    _same_but(torch, pre, pre2, rows)
+    wc, ws = mb.molora_mx_quantize_w(W)
+    _same_but(torch, mb.molora_apply_mx(x, wc, ws, A, B, rd), mb.molora_apply_mx(x2, wc, ws, A, B, rd), rows)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    dz = torch.randn(N, F, generator=g, device="cuda").bfloat16()
+    dz2 = dz.clone()
+    dz2[0, F - 1] = float("nan")
+    clean, got = (mb.molora_gated_backward(t, x, W, A, B, rd, pre) for t in (dz, dz2))
+    rows[N - 1] = False
+    _same_but(torch, clean[0], got[0], rows)
+    keep = [c for c in range(C) if c != r[0]]
+    assert torch.equal(clean[2][keep], got[2][keep]) and torch.equal(clean[3][keep], got[3][keep])
+    assert not bool(torch.isfinite(got[1].float()).all())
