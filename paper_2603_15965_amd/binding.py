@@ -287,12 +287,31 @@ def _opt(t, dtype, name, shape=None):
     return None if t is None else _dev(t, dtype, name, shape)
 
 
+def _empty(shape, dtype, device, stream):
+    """What a call on `stream` writes and the caller did not hand in, from that stream's memory (as under
+    torch.cuda.stream(stream)): a block of the current stream may still be in use by kernels there that nothing
+    orders before this call's, and given back early it would go to kernels that nothing orders behind them."""
+    if stream is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+    else:
+        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+            t = torch.empty(shape, dtype=dtype, device=device)
+    if _recording:   # what a recorded call writes to belongs to its graph: every replay writes there
+        graph = _recording.get(_stream_now(stream))
+        if graph is not None:
+            graph._memory.append(t)
+    return t
+
+
+_recording = {}   # stream handle -> the Graph that records it
+
+
 def molora_route(x, G, r=None, stream=None):
     """r[i] = argmax_c x[i] . G[:, c] (fp32 ascending-k chain, lowest index on ties)."""
     N, d_in = _two(x, "x")
     C = _two(G, "G")[1]
     if r is None:
-        r = torch.empty(N, dtype=torch.int32, device=x.device)
+        r = _empty(N, torch.int32, x.device, stream)
     _call("molora_route", _dev(x, torch.bfloat16, "x"), _dev(G, torch.bfloat16, "G", (d_in, C)),
                              _dev(r, torch.int32, "r", (N,)), N, d_in, C, _stream(stream))
     return r
@@ -303,7 +322,7 @@ def molora_route_vocab(v, breaks, r=None, stream=None):
     N = int(v.shape[0])
     arr, M = _breaks(breaks)
     if r is None:
-        r = torch.empty(N, dtype=torch.int32, device=v.device)
+        r = _empty(N, torch.int32, v.device, stream)
     _call("molora_route_vocab", _dev(v, torch.int32, "v", (N,)), arr, M, _dev(r, torch.int32, "r", (N,)), N,
                                    _stream(stream))
     return r
@@ -314,9 +333,9 @@ def molora_bucket(r, C, offsets=None, perm=None, err_flag=None, stream=None):
     N = int(r.shape[0])
     C = int(C)
     if offsets is None:
-        offsets = torch.empty(C + 1, dtype=torch.int32, device=r.device)
+        offsets = _empty(C + 1, torch.int32, r.device, stream)
     if perm is None:
-        perm = torch.empty(max(N, 1), dtype=torch.int32, device=r.device)[:N]
+        perm = _empty(max(N, 1), torch.int32, r.device, stream)[:N]
     _call("molora_bucket", _dev(r, torch.int32, "r", (N,)), _dev(offsets, torch.int32, "offsets", (C + 1,)),
                               _dev(perm, torch.int32, "perm", (N,)), N, C,
                               _opt(err_flag, torch.int32, "err_flag"), _stream(stream))
@@ -337,9 +356,9 @@ def _shapes(x, W, A, B):
     return N, d_in, d_out, C, rank
 
 
-def new_workspace(N, d_in, d_out, C, rank, device="cuda"):
+def new_workspace(N, d_in, d_out, C, rank, device="cuda", stream=None):
     nbytes = molora_apply_workspace_bytes(N, d_in, d_out, C, rank)
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    return _empty(max(nbytes, 256), torch.uint8, device, stream)
 
 
 def _flat_bytes(t, name):
@@ -352,9 +371,9 @@ def molora_apply(x, W, A, B, r, h=None, workspace=None, stream=None):
     """h[i] = x[i] W + (x[i] A[r[i]]) B[r[i]]  (fp32 [N][d_out])."""
     N, d_in, d_out, C, rank = _shapes(x, W, A, B)
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     if workspace is None:
-        workspace = new_workspace(N, d_in, d_out, C, rank, x.device)
+        workspace = new_workspace(N, d_in, d_out, C, rank, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = _flat_bytes(workspace, "workspace")
     _call("molora_apply", _dev(x, bf, "x"), _dev(W, bf, "W"), _dev(A, bf, "A"), _dev(B, bf, "B"),
@@ -379,9 +398,9 @@ def molora_apply_bucketed(x, W, A, B, offsets, perm, h=None, workspace=None, str
     """molora_apply for a caller that already holds molora_bucket's output."""
     N, d_in, d_out, C, rank = _shapes(x, W, A, B)
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     if workspace is None:
-        workspace = new_workspace(N, d_in, d_out, C, rank, x.device)
+        workspace = new_workspace(N, d_in, d_out, C, rank, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = _flat_bytes(workspace, "workspace")
     _call("molora_apply_bucketed", 
@@ -391,10 +410,10 @@ def molora_apply_bucketed(x, W, A, B, offsets, perm, h=None, workspace=None, str
     return h
 
 
-def molora_shrink_workspace(N, d_in, C, rank, device="cuda"):
+def molora_shrink_workspace(N, d_in, C, rank, device="cuda", stream=None):
     """Scratch for molora_shrink (None when these sizes need none)."""
     nbytes = int(load().molora_shrink_workspace_bytes(N, d_in, C, rank))
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    return _empty(nbytes, torch.uint8, device, stream) if nbytes else None
 
 
 def molora_shrink(x, A, offsets, perm, t=None, workspace="auto", stream=None):
@@ -403,9 +422,9 @@ def molora_shrink(x, A, offsets, perm, t=None, workspace="auto", stream=None):
     N, d_in = _two(x, "x")
     C, _, rank = _three(A, "A")
     if t is None:
-        t = torch.empty((N, 2 * rank), dtype=torch.bfloat16, device=x.device)
+        t = _empty((N, 2 * rank), torch.bfloat16, x.device, stream)
     if isinstance(workspace, str):
-        workspace = molora_shrink_workspace(N, d_in, C, rank, x.device)
+        workspace = molora_shrink_workspace(N, d_in, C, rank, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = (None, 0) if workspace is None else _flat_bytes(workspace, "workspace")
     _call("molora_shrink", _dev(x, bf, "x"), _dev(A, bf, "A", (C, d_in, rank)),
@@ -415,12 +434,12 @@ def molora_shrink(x, A, offsets, perm, t=None, workspace="auto", stream=None):
     return t
 
 
-def _base_expand_args(x, W, B, t, offsets, perm, h, t_cols):
+def _base_expand_args(x, W, B, t, offsets, perm, h, t_cols, stream):
     N, d_in = _two(x, "x")
     d_out = _two(W, "W")[1]
     C, rank, _ = _three(B, "B")
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     bf = torch.bfloat16
     args = [_dev(x, bf, "x"), _dev(W, bf, "W", (d_in, d_out)), _dev(B, bf, "B", (C, rank, d_out)),
             _dev(t, bf, "t", (N, t_cols(C, rank))), _dev(offsets, torch.int32, "offsets", (C + 1,)),
@@ -432,7 +451,7 @@ def _base_expand_args(x, W, B, t, offsets, perm, h, t_cols):
 def molora_base_expand(x, W, B, t, offsets, perm, h=None, stream=None, tile_rows=None):
     """h[perm[p]] = x[perm[p]] W + t_p B_c, every row written once.  tile_rows (64, 128 or
     256) forces the row-tile height (molora_base_expand_fixed, for the tiling ablation)."""
-    args, h = _base_expand_args(x, W, B, t, offsets, perm, h, lambda C, rank: 2 * rank)
+    args, h = _base_expand_args(x, W, B, t, offsets, perm, h, lambda C, rank: 2 * rank, stream)
     if tile_rows is None:
         _call("molora_base_expand", *args, _stream(stream))
     else:
@@ -453,13 +472,13 @@ def molora_dense_shrink_supported(N, d_in, C, rank):
     return bool(load().molora_dense_shrink_supported(N, d_in, C, rank))
 
 
-def _dense_outputs(N, C, rank, offsets, perm, t, device):
+def _dense_outputs(N, C, rank, offsets, perm, t, device, stream):
     if offsets is None:
-        offsets = torch.empty(C + 1, dtype=torch.int32, device=device)
+        offsets = _empty(C + 1, torch.int32, device, stream)
     if perm is None:
-        perm = torch.empty(N, dtype=torch.int32, device=device)
+        perm = _empty(N, torch.int32, device, stream)
     if t is None:
-        t = torch.empty((N, 2 * C * rank), dtype=torch.bfloat16, device=device)
+        t = _empty((N, 2 * C * rank), torch.bfloat16, device, stream)
     return offsets, perm, t
 
 
@@ -467,7 +486,7 @@ def molora_bucket_shrink(r, x, A, offsets=None, perm=None, t=None, err_flag=None
     """Dispatch (r given) and token-order shrink in one launch: (offsets, perm, t [N][2*C*rank])."""
     N, d_in = _two(x, "x")
     C, _, rank = _three(A, "A")
-    offsets, perm, t = _dense_outputs(N, C, rank, offsets, perm, t, x.device)
+    offsets, perm, t = _dense_outputs(N, C, rank, offsets, perm, t, x.device, stream)
     bf = torch.bfloat16
     _call("molora_bucket_shrink", _dev(r, torch.int32, "r", (N,)), _dev(x, bf, "x"),
                                      _dev(A, bf, "A", (C, d_in, rank)),
@@ -490,13 +509,13 @@ def molora_bucket_shrink_small(r, x, A, offsets=None, perm=None, t=None, workspa
     N, d_in = _two(x, "x")
     C, _, rank = _three(A, "A")
     if offsets is None:
-        offsets = torch.empty(C + 1, dtype=torch.int32, device=x.device)
+        offsets = _empty(C + 1, torch.int32, x.device, stream)
     if perm is None:
-        perm = torch.empty(N, dtype=torch.int32, device=x.device)
+        perm = _empty(N, torch.int32, x.device, stream)
     if t is None:
-        t = torch.empty((N, 2 * rank), dtype=torch.bfloat16, device=x.device)
+        t = _empty((N, 2 * rank), torch.bfloat16, x.device, stream)
     if isinstance(workspace, str):
-        workspace = molora_shrink_workspace(N, d_in, C, rank, x.device)
+        workspace = molora_shrink_workspace(N, d_in, C, rank, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = (None, 0) if workspace is None else _flat_bytes(workspace, "workspace")
     _call("molora_bucket_shrink_small", _dev(r, torch.int32, "r", (N,)), _dev(x, bf, "x"),
@@ -519,7 +538,7 @@ def molora_pack_w(W, Wp=None, stream=None):
     if molora_pack_w_cols(d_out) == 0:
         raise ValueError(f"a base weight with {d_out} columns has no packed form")
     if Wp is None:
-        Wp = torch.empty_like(W)
+        Wp = _empty(W.shape, W.dtype, W.device, stream)
     bf = torch.bfloat16
     _call("molora_pack_w", _dev(W, bf, "W"), _dev(Wp, bf, "Wp", (d_in, d_out)), d_in, d_out, _stream(stream))
     return Wp
@@ -536,13 +555,13 @@ def molora_shrink_base_small(r, x, W, A, offsets=None, perm=None, t=None, h=None
         raise ValueError(f"a base weight with {d_out} columns has no packed form")
     C, _, rank = _three(A, "A")
     if offsets is None:
-        offsets = torch.empty(C + 1, dtype=torch.int32, device=x.device)
+        offsets = _empty(C + 1, torch.int32, x.device, stream)
     if perm is None:
-        perm = torch.empty(N, dtype=torch.int32, device=x.device)
+        perm = _empty(N, torch.int32, x.device, stream)
     if t is None:
-        t = torch.empty((N, 2 * rank), dtype=torch.bfloat16, device=x.device)
+        t = _empty((N, 2 * rank), torch.bfloat16, x.device, stream)
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     bf = torch.bfloat16
     _call("molora_shrink_base_small_packed" if packed else "molora_shrink_base_small",
           _dev(r, torch.int32, "r", (N,)), _dev(x, bf, "x"),
@@ -560,7 +579,7 @@ def molora_pack_b(B, Bp=None, stream=None):
     if rank % 16 != 0:
         raise ValueError(f"a packed B needs a rank that is a multiple of 16, not {rank}")
     if Bp is None:
-        Bp = torch.empty_like(B)
+        Bp = _empty(B.shape, B.dtype, B.device, stream)
     _three(Bp, "Bp")
     if tuple(Bp.shape) != tuple(B.shape):
         raise ValueError(f"Bp has shape {tuple(Bp.shape)}, B {tuple(B.shape)}")
@@ -593,8 +612,8 @@ def molora_gate_dispatch_shrink(v, breaks, x, A, adapter=None, n_adapters=1, r=N
     if C != n_adapters * M:
         raise ValueError("A must hold n_adapters * M adapters")
     if r is None:
-        r = torch.empty(N, dtype=torch.int32, device=x.device)
-    offsets, perm, t = _dense_outputs(N, C, rank, offsets, perm, t, x.device)
+        r = _empty(N, torch.int32, x.device, stream)
+    offsets, perm, t = _dense_outputs(N, C, rank, offsets, perm, t, x.device, stream)
     bf = torch.bfloat16
     _call("molora_gate_dispatch_shrink", 
         _dev(v, torch.int32, "v", (N,)), _opt(adapter, torch.int32, "adapter", (N,)), arr, M,
@@ -607,7 +626,7 @@ def molora_gate_dispatch_shrink(v, breaks, x, A, adapter=None, n_adapters=1, r=N
 
 def molora_base_expand_dense(x, W, B, t, offsets, perm, h=None, stream=None):
     """molora_base_expand reading the token-order intermediate of the two calls above."""
-    args, h = _base_expand_args(x, W, B, t, offsets, perm, h, lambda C, rank: 2 * C * rank)
+    args, h = _base_expand_args(x, W, B, t, offsets, perm, h, lambda C, rank: 2 * C * rank, stream)
     _call("molora_base_expand_dense", *args, _stream(stream))
     return h
 
@@ -634,12 +653,12 @@ def molora_route_mlp(x, W1, b1, W2, b2, k, idx=None, w=None, workspace=None, str
     H, K = _two(W2, "W2")
     k = int(k)
     if idx is None:
-        idx = torch.empty((N, k), dtype=torch.int32, device=x.device)
+        idx = _empty((N, k), torch.int32, x.device, stream)
     if w is None:
-        w = torch.empty((N, k), dtype=torch.float32, device=x.device)
+        w = _empty((N, k), torch.float32, x.device, stream)
     if workspace is None:
         nbytes = int(load().molora_route_mlp_workspace_bytes(N, H))
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=x.device)
+        workspace = _empty(max(nbytes, 256), torch.uint8, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = _flat_bytes(workspace, "workspace")
     _call("molora_route_mlp", _dev(x, bf, "x"), _dev(W1, bf, "W1", (d_in, H)),
@@ -655,7 +674,7 @@ def molora_route_compose(v, adapter, breaks, n_adapters, r=None, stream=None):
     N = int(v.shape[0])
     arr, M = _breaks(breaks)
     if r is None:
-        r = torch.empty(N, dtype=torch.int32, device=v.device)
+        r = _empty(N, torch.int32, v.device, stream)
     _call("molora_route_compose", _dev(v, torch.int32, "v", (N,)), _dev(adapter, torch.int32, "adapter", (N,)),
                                      arr, M, n_adapters, _dev(r, torch.int32, "r", (N,)), N, _stream(stream))
     return r
@@ -668,11 +687,11 @@ def molora_gate_dispatch(v, breaks, adapter=None, n_adapters=1, r=None, offsets=
     arr, M = _breaks(breaks)
     C = n_adapters * M
     if r is None:
-        r = torch.empty(N, dtype=torch.int32, device=v.device)
+        r = _empty(N, torch.int32, v.device, stream)
     if offsets is None:
-        offsets = torch.empty(C + 1, dtype=torch.int32, device=v.device)
+        offsets = _empty(C + 1, torch.int32, v.device, stream)
     if perm is None:
-        perm = torch.empty(max(N, 1), dtype=torch.int32, device=v.device)[:N]
+        perm = _empty(max(N, 1), torch.int32, v.device, stream)[:N]
     _call("molora_gate_dispatch", 
         _dev(v, torch.int32, "v", (N,)), _opt(adapter, torch.int32, "adapter", (N,)),
         arr, M, n_adapters, _dev(r, torch.int32, "r", (N,)), _dev(offsets, torch.int32, "offsets", (C + 1,)),
@@ -692,10 +711,10 @@ def molora_apply_mix(x, W, A, B, idx, w=None, slots=None, C=None, h=None, worksp
     if slots is None and C > S:
         raise ValueError("without a slot table the adapter indices address the pool: C <= pool size")
     if h is None:
-        h = torch.empty((N, d_out), dtype=torch.float32, device=x.device)
+        h = _empty((N, d_out), torch.float32, x.device, stream)
     if workspace is None:
         nbytes = int(load().molora_apply_mix_workspace_bytes(N, d_in, d_out, C, rank, k))
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=x.device)
+        workspace = _empty(max(nbytes, 256), torch.uint8, x.device, stream)
     bf = torch.bfloat16
     ws, ws_bytes = _flat_bytes(workspace, "workspace")
     _call("molora_apply_mix", 
@@ -735,25 +754,6 @@ def _mx_shapes(rows, K):
         raise ValueError(f"a microscaled operand has K >= 8, a multiple of 8, and less than 2^31 either way: got {rows} rows of {K}")
     tiles = -(-rows // 16)
     return (tiles, -(-K // 128), 64, 16), (tiles, -(-K // 512), 64, 4)
-
-
-def _empty(shape, dtype, device, stream):
-    """What a call on `stream` writes and the caller did not hand in, from that stream's memory (as under
-    torch.cuda.stream(stream)): a block of the current stream may still be in use by kernels there that nothing
-    orders before this call's, and given back early it would go to kernels that nothing orders behind them."""
-    if stream is None:
-        t = torch.empty(shape, dtype=dtype, device=device)
-    else:
-        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
-            t = torch.empty(shape, dtype=dtype, device=device)
-    if _recording:   # what a recorded call writes to belongs to its graph: every replay writes there
-        graph = _recording.get(_stream_now(stream))
-        if graph is not None:
-            graph._memory.append(t)
-    return t
-
-
-_recording = {}   # stream handle -> the Graph that records it
 
 
 def _mx_outputs(rows, K, codes, scales, like, stream):
@@ -926,8 +926,7 @@ class Graph:
             molora_route(..., stream=stream); molora_bucket(..., stream=stream); ...
         g.launch()                   # replays on `stream`
 
-    The calls of the feed-forward block may allocate outputs and workspaces while they are recorded: the graph keeps
-    that memory until it is destroyed.  The other calls want theirs from the caller, who keeps it.
+    Calls may allocate outputs and workspaces while they are recorded: the graph keeps that memory until it is destroyed.
     """
 
     def __init__(self, stream):
